@@ -202,6 +202,115 @@ masq_status masq_mas_only_linear(const void* x, masq_dtype x_dt, const int32_t* 
 size_t masq_mas_only_workspace_bytes(int64_t T, int64_t c_in, int64_t c_out, int32_t n_mod);
 
 /*
+ * What follows the layer in a decoder block, in the epilogue of its product:
+ * with z the fp32 output of masq_linear_fused before its rounding,
+ *     z_o += bias[o]                                  (bias: f32, nullable)
+ *     h_o  = act(z_o)                  o < c_out, or, with MASQ_ACT_GATED,
+ *     h_i  = act(z_2i) * z_2i+1        i < c_out / 2  (gate and up channels)
+ *     y    = h + residual                             (nullable)
+ * in fp32, rounded once into y's dtype.  act is a masq_act, plus
+ * MASQ_ACT_GATED for channels in pairs: rows 2i and 2i + 1 of wq (and of
+ * w_scale, r_up and bias) are output i's gate and up channels, c_out counts
+ * both and is a multiple of 32, and rows of y and residual have c_out / 2
+ * outputs.  residual is in y's dtype and y's shape and may be y itself.
+ * weight_bits: 8 (wq as for masq_linear_fused) or 4 (packed, as for
+ * masq_linear_fused_w4a8).  Text rows without bias, activation and residual
+ * are masq_linear_fused's bit for bit.  Other arguments, preconditions, errors
+ * and the workspace are masq_linear_fused's (_w4a8's); an unknown act is
+ * MASQ_ERR_UNSUPPORTED.
+ */
+typedef enum {
+    MASQ_ACT_NONE = 0,
+    MASQ_ACT_SILU = 1,        /* z / (1 + exp(-z))                               */
+    MASQ_ACT_GELU = 2,        /* z Phi(z), with the error function               */
+    MASQ_ACT_GELU_TANH = 3,   /* z (1 + tanh(sqrt(2/pi)(z + 0.044715 z^3))) / 2  */
+    MASQ_ACT_GATED = 16       /* added to one of the above                       */
+} masq_act;
+
+masq_status masq_linear_epilogue(const void* x, masq_dtype x_dt, const int32_t* modality,
+                                 const float* inv_smooth, const void* wq, int32_t weight_bits,
+                                 const float* w_scale, const void* l_down, const void* r_up,
+                                 masq_dtype lr_dt, int64_t T, int64_t c_in, int64_t c_out,
+                                 int32_t rank, int32_t n_mod, const float* bias, int32_t act,
+                                 const void* residual, void* y, masq_dtype y_dt, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * The layer in a mixture of experts.
+ *
+ * masq_route_experts: every token's top_k experts and the choices of all
+ * tokens sorted by expert.  logits [T][n_experts] f32 or bf16.  A token
+ * chooses its largest logits, largest first, ties to the lowest index; a logit
+ * of -inf or NaN is never chosen, so a row of -inf (padding) chooses nothing
+ * and a row with fewer others than top_k chooses those.
+ *   experts [T][top_k]: the choices; -1 where there is none
+ *   weights [T][top_k] f32: softmax of the row's logits at the choices, over
+ *       the chosen ones (renormalize != 0) or over all n_experts; 0 where
+ *       there is no choice.  (+inf logits share the weight equally.)
+ *   offsets [n_experts + 1]: expert e's slots are offsets[e] ..
+ *       offsets[e + 1] - 1; offsets[n_experts] is the number of choices
+ *   rows [T top_k]: the token of each slot, ascending inside an expert; -1
+ *       past the last choice
+ *   slots [T][top_k]: the slot of each choice; -1 where there is none
+ *   slot_modality [T top_k] (given with modality [T], or both NULL): the
+ *       modality of each slot's token, 0 past the last choice
+ * 1 <= n_experts <= 512, 1 <= top_k <= min(n_experts, 16), T top_k < 2^31.
+ * workspace: masq_route_experts_workspace_bytes(...) bytes (0 for small
+ * batches: may then be NULL), 256-byte aligned, contents need not be
+ * initialised, not shared by concurrent calls.
+ *
+ * masq_expert_linear: masq_linear_epilogue (without residual) with weights,
+ * scales, compensation factors and bias of the slot's expert: for each slot p
+ * in [offsets[e], offsets[e + 1]) with t = rows[p] (rows == NULL: t = p, and
+ * n_slots == T: x is in slot order),
+ *     z_p = (float(Q(x_t S_m^-1) . wq[e]^T) * delta_t) * w_scale[e]
+ *           + [m != text] (x_t S_m^-1) L1_e^m L2_e^m,    m = modality[t]
+ * then bias[e], activation and gating as above, into row p of y.  Rows of y
+ * past offsets[n_experts] are left as they were.  The smoothing factors are
+ * the experts' common ones, so a token is quantised once.
+ *   x [T][c_in], modality [T], inv_smooth [n_mod][c_in]
+ *   wq [n_experts][c_out][c_in] int8 (weight_bits 8) or [..][c_in / 2] packed
+ *   w_scale, bias (nullable) [n_experts][c_out] f32
+ *   l_down [n_experts][n_mod-1][rank][c_in], r_up [n_experts][n_mod-1][c_out][rank]
+ *   rows [n_slots] in [0, T) at the experts' slots, offsets [n_experts + 1]
+ *   ascending in [0, n_slots]: DEVICE arrays that the host never reads.
+ *   (Other values are memory-safe, but not a supported input: rows outside
+ *   [0, T) read row 0, offsets are clamped.)
+ *   y [n_slots][c_out, or c_out / 2 where gated]
+ * T == 0 or n_slots == 0 is a no-op.  workspace:
+ * masq_expert_linear_workspace_bytes(...) bytes, 256-byte aligned, not shared
+ * by concurrent calls.  n_experts <= 512, n_slots < 2^31 (and fewer than 2^31
+ * output tiles); other preconditions and errors as masq_linear_epilogue.
+ *
+ * masq_combine_experts: y[t] = residual[t] (nullable) + sum over j < top_k of
+ * weights[t][j] d[slots[t][j]], summed in fp32 in the order of j, then the
+ * residual, rounded once.  d [n_slots][c_out], y and residual [T][c_out] in
+ * one dtype; residual may be y itself.  A slot outside [0, n_slots) adds
+ * nothing (d may be NULL with n_slots == 0).  c_out % 16 == 0, top_k <= 16.
+ */
+masq_status masq_route_experts(const void* logits, masq_dtype dt, const int32_t* modality, int64_t T,
+                               int32_t n_experts, int32_t top_k, int32_t renormalize,
+                               int32_t* experts, float* weights, int32_t* offsets, int32_t* rows,
+                               int32_t* slots, int32_t* slot_modality, void* workspace,
+                               size_t workspace_bytes, void* stream);
+size_t masq_route_experts_workspace_bytes(int64_t T, int32_t n_experts);
+
+masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const int32_t* modality,
+                               const float* inv_smooth, const void* wq, int32_t weight_bits,
+                               const float* w_scale, const void* l_down, const void* r_up,
+                               masq_dtype lr_dt, const int32_t* rows, const int32_t* offsets,
+                               int64_t n_slots, int32_t n_experts, int64_t c_in, int64_t c_out,
+                               int32_t rank, int32_t n_mod, const float* bias, int32_t act, void* y,
+                               masq_dtype y_dt, void* workspace, size_t workspace_bytes,
+                               void* stream);
+size_t masq_expert_linear_workspace_bytes(int64_t T, int64_t n_slots, int64_t c_in, int32_t rank,
+                                          int32_t n_mod);
+
+masq_status masq_combine_experts(const void* d, masq_dtype dt, const int32_t* slots,
+                                 const float* weights, int64_t T, int64_t n_slots, int64_t c_out,
+                                 int32_t top_k, const void* residual, void* y, void* stream);
+
+/*
  * The two launch stages masq_linear_fused is made of, with identical
  * arguments, exposed so that a caller can place events or other stream work
  * between them.  stage1: smoothing, quantisation and the rank-r

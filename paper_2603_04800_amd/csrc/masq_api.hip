@@ -276,6 +276,39 @@ MasOnlyWs plan_mas_only(void* base, int64_t T, int64_t K, int64_t N, int n_mod) 
     return w;
 }
 
+// Workspace of the experts' layer: plain codes and scales of x's rows, and (with
+// a compensation) u by slot.
+struct ExpertWs {
+    int8_t* q;
+    float* x_scale;
+    float* u;
+    size_t bytes;
+};
+
+ExpertWs plan_experts(void* base, int64_t T, int64_t n_slots, int64_t K, int rank, int n_mod) {
+    ExpertWs w{};
+    size_t off = 0;
+    uint8_t* b = static_cast<uint8_t*>(base);
+    auto carve = [&](size_t bytes) {
+        uint8_t* p = b ? b + off : nullptr;
+        off += align256(bytes);
+        return p;
+    };
+    w.q = reinterpret_cast<int8_t*>(carve(static_cast<size_t>(T) * static_cast<size_t>(K)));
+    w.x_scale = reinterpret_cast<float*>(carve(static_cast<size_t>(T) * sizeof(float)));
+    if (rank > 0 && n_mod > 1)
+        w.u = reinterpret_cast<float*>(carve(static_cast<size_t>(n_slots) * rank * sizeof(float)));
+    w.bytes = off;
+    return w;
+}
+
+// Tile shape of the experts' layer: 32-row tiles for up to 16 rows an expert
+// on average, 64-row tiles up to 64, else 128 x 128.
+TilePlan plan_expert_tile(int64_t n_slots, int64_t n_experts) {
+    const int64_t avg = n_slots / n_experts;
+    return TilePlan{avg <= 16 ? 0 : (avg <= 64 ? 1 : 2), 1};
+}
+
 }  // namespace masq
 
 using masq::DT;
@@ -322,7 +355,15 @@ struct Fused {
     masq_dtype lr_dt; int64_t T, c_in, c_out; int32_t rank, n_mod; void* y; masq_dtype y_dt;
     void* workspace; size_t workspace_bytes; void* stream;
     bool w4;      // wq: packed 4-bit codes, [c_out][c_in / 2] bytes
+    const masq::TileExtra* ex = nullptr;   // bias, activation and residual past the layer
 };
+
+// The activation argument: kind and gating bit.
+masq_status check_act(int32_t act, int64_t c_out) {
+    const int32_t kind = act & ~MASQ_ACT_GATED;
+    if (kind < MASQ_ACT_NONE || kind > MASQ_ACT_GELU_TANH) return MASQ_ERR_UNSUPPORTED;
+    return (act & MASQ_ACT_GATED) != 0 && c_out % 32 != 0 ? MASQ_ERR_SHAPE : MASQ_OK;
+}
 
 masq_status validate_fused(const Fused& a) {
     masq_status st = check_dims(a.T, a.c_in, a.c_out, true);
@@ -419,6 +460,23 @@ masq_status fused_stage(const Fused& a, int stage) {
         // the hi/lo rows of u exist when the fused stage 1 wrote them
         const bool hl = cmc && !masq::small_path(a.T, a.c_in) &&
                         masq::fused_stage1_ok(a.T, a.c_in, a.rank, to_dt(a.lr_dt));
+        if (a.ex != nullptr) {
+            const bool parts = w.u_part != nullptr && w.n_kslices > 1;
+            if (masq::small_path(a.T, a.c_in))
+                return from_hip(masq::launch_gemm_stream_epilogue(
+                    masq::StreamGemm{w.q, w.x_scale, a.wq, a.w_scale, a.T, a.c_in, a.c_out, a.modality,
+                                     cmc ? (parts ? w.u_part : w.u) : nullptr, parts ? w.n_kslices : 1,
+                                     a.rank, a.n_mod, a.r_up, to_dt(a.lr_dt), a.y, to_dt(a.y_dt), a.w4,
+                                     w.dec_part, w.dec_tickets, -1, s},
+                    *a.ex));
+            return from_hip(masq::launch_gemm_tile_epilogue(
+                masq::TileGemm{w.q, w.x_scale, a.wq, a.w_scale, a.T, a.c_in, a.c_out, a.modality, w.u,
+                               hl ? w.u_hl : nullptr, a.rank, a.n_mod, a.r_up, to_dt(a.lr_dt), cmc,
+                               nullptr, a.y, to_dt(a.y_dt), a.w4, w.pair,
+                               w.tile.shape >= 0 ? w.tile : masq::TilePlan{2, 1}, w.gk_part,
+                               w.gk_tickets, s},
+                *a.ex));
+        }
         st = from_hip(masq::launch_gemm(w.q, w.x_scale, a.wq, a.w_scale, a.T, a.c_in, a.c_out,
                                         a.modality, w.u, hl ? w.u_hl : nullptr, w.dec_part,
                                         w.dec_tickets, w.gk_splits, w.gk_part, w.gk_tickets,
@@ -652,6 +710,156 @@ masq_status masq_linear_stage1_w4a8(MASQ_FUSED_ARGS_W4) {
 }
 masq_status masq_linear_stage2_w4a8(MASQ_FUSED_ARGS_W4) {
     return fused_stage(MASQ_FUSED_PACK(MASQ_W4, true), 2);
+}
+
+masq_status masq_linear_epilogue(const void* x, masq_dtype x_dt, const int32_t* modality,
+                                 const float* inv_smooth, const void* wq, int32_t weight_bits,
+                                 const float* w_scale, const void* l_down, const void* r_up,
+                                 masq_dtype lr_dt, int64_t T, int64_t c_in, int64_t c_out,
+                                 int32_t rank, int32_t n_mod, const float* bias, int32_t act,
+                                 const void* residual, void* y, masq_dtype y_dt, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+    if (weight_bits != 8 && weight_bits != 4) return MASQ_ERR_SHAPE;
+    Fused a{x, x_dt, modality, inv_smooth, static_cast<const int8_t*>(wq), w_scale, l_down, r_up, lr_dt,
+            T, c_in, c_out, rank, n_mod, y, y_dt, workspace, workspace_bytes, stream, weight_bits == 4};
+    masq_status st = check_act(act, c_out);
+    if (st != MASQ_OK) return st;
+    if ((st = validate_fused(a)) != MASQ_OK || T == 0) return st;
+    if ((bias && !aligned16(bias)) || (residual && !aligned16(residual))) return MASQ_ERR_ALIGN;
+    masq::TileExtra ex{};
+    ex.bias = bias;
+    ex.residual = residual;
+    ex.act = act & ~MASQ_ACT_GATED;
+    ex.gated = (act & MASQ_ACT_GATED) != 0;
+    a.ex = &ex;
+    return fused_stage(a, 3);
+}
+
+static masq_status check_experts(int32_t n_experts) {
+    return n_experts < 1 || n_experts > masq::kRouteMaxExperts ? MASQ_ERR_SHAPE : MASQ_OK;
+}
+
+static masq_status check_route(int64_t T, int32_t n_experts, int32_t top_k) {
+    if (T < 0 || check_experts(n_experts) != MASQ_OK) return MASQ_ERR_SHAPE;
+    if (top_k < 1 || top_k > masq::kRouteMaxK || top_k > n_experts) return MASQ_ERR_SHAPE;
+    return T > ((1LL << 31) - 1) / top_k ? MASQ_ERR_SHAPE : MASQ_OK;
+}
+
+size_t masq_route_experts_workspace_bytes(int64_t T, int32_t n_experts) {
+    if (T < 0 || check_experts(n_experts) != MASQ_OK) return 0;
+    return masq::plan_route(nullptr, T, n_experts).bytes;
+}
+
+masq_status masq_route_experts(const void* logits, masq_dtype dt, const int32_t* modality, int64_t T,
+                               int32_t n_experts, int32_t top_k, int32_t renormalize,
+                               int32_t* experts, float* weights, int32_t* offsets, int32_t* rows,
+                               int32_t* slots, int32_t* slot_modality, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    masq_status st = check_route(T, n_experts, top_k);
+    if (st != MASQ_OK) return st;
+    if (!valid_dt(dt)) return MASQ_ERR_DTYPE;
+    if (T == 0) return MASQ_OK;
+    if (!logits || !experts || !weights || !offsets || !rows || !slots) return MASQ_ERR_NULL;
+    if ((modality == nullptr) != (slot_modality == nullptr)) return MASQ_ERR_NULL;
+    const void* ptrs[] = {logits, experts, weights, offsets, rows, slots, modality, slot_modality};
+    for (const void* p : ptrs)
+        if (!aligned16(p)) return MASQ_ERR_ALIGN;
+    const masq::RouteWs w = masq::plan_route(workspace, T, n_experts);
+    if (w.bytes > 0) {
+        if (!workspace) return MASQ_ERR_NULL;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return MASQ_ERR_ALIGN;
+        if (workspace_bytes < w.bytes) return MASQ_ERR_WORKSPACE;
+    }
+    (void)hipGetLastError();
+    return from_hip(masq::launch_route(logits, to_dt(dt), modality, T, n_experts, top_k,
+                                       renormalize != 0, experts, weights, offsets, rows, slots,
+                                       slot_modality, w, static_cast<hipStream_t>(stream)));
+}
+
+size_t masq_expert_linear_workspace_bytes(int64_t T, int64_t n_slots, int64_t c_in, int32_t rank,
+                                          int32_t n_mod) {
+    if (T < 0 || n_slots < 0 || c_in <= 0 || rank < 0) return 0;
+    return masq::plan_experts(nullptr, T, n_slots, c_in, rank, n_mod).bytes;
+}
+
+masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const int32_t* modality,
+                               const float* inv_smooth, const void* wq, int32_t weight_bits,
+                               const float* w_scale, const void* l_down, const void* r_up,
+                               masq_dtype lr_dt, const int32_t* rows, const int32_t* offsets,
+                               int64_t n_slots, int32_t n_experts, int64_t c_in, int64_t c_out,
+                               int32_t rank, int32_t n_mod, const float* bias, int32_t act, void* y,
+                               masq_dtype y_dt, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    masq_status st = check_dims(T, c_in, c_out, true);
+    if (st != MASQ_OK) return st;
+    if (weight_bits != 8 && weight_bits != 4) return MASQ_ERR_SHAPE;
+    const bool w4 = weight_bits == 4;
+    if (w4 && c_in % 64 != 0) return MASQ_ERR_SHAPE;
+    if ((st = check_exact_acc(c_in, w4)) != MASQ_OK) return st;
+    if ((st = check_rank(rank, n_mod)) != MASQ_OK) return st;
+    if ((st = check_experts(n_experts)) != MASQ_OK) return st;
+    if ((st = check_act(act, c_out)) != MASQ_OK) return st;
+    if (n_slots < 0 || n_slots > (1LL << 31) - 1) return MASQ_ERR_SHAPE;
+    if (rows == nullptr && n_slots > 0 && T > 0 && n_slots != T) return MASQ_ERR_SHAPE;
+    const masq::TilePlan plan = masq::plan_expert_tile(n_slots, n_experts);
+    // tiles are counted in 32 bits
+    const int64_t tiles = masq::expert_tiles(n_slots, n_experts, masq::kTileShapes[plan.shape].bm);
+    const int64_t tiles_n = (c_out + masq::kTileShapes[plan.shape].bn - 1) / masq::kTileShapes[plan.shape].bn;
+    if (tiles > ((1LL << 31) - 8) / tiles_n) return MASQ_ERR_SHAPE;
+    if (!valid_dt(x_dt) || !valid_dt(y_dt) || !valid_dt(lr_dt)) return MASQ_ERR_DTYPE;
+    if (T == 0 || n_slots == 0) return MASQ_OK;
+    const bool cmc = rank > 0 && n_mod > 1;
+    if (!x || !modality || !inv_smooth || !wq || !w_scale || !offsets || !y || !workspace)
+        return MASQ_ERR_NULL;
+    if (cmc && (!l_down || !r_up)) return MASQ_ERR_NULL;
+    const void* ptrs[] = {x, modality, inv_smooth, wq, w_scale, rows, offsets, bias, y,
+                          cmc ? l_down : nullptr, cmc ? r_up : nullptr};
+    for (const void* p : ptrs)
+        if (!aligned16(p)) return MASQ_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return MASQ_ERR_ALIGN;
+    const masq::ExpertWs w = masq::plan_experts(workspace, T, n_slots, c_in, rank, n_mod);
+    if (workspace_bytes < w.bytes) return MASQ_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    masq::TileExtra ex{};
+    ex.bias = bias;
+    ex.act = act & ~MASQ_ACT_GATED;
+    ex.gated = (act & MASQ_ACT_GATED) != 0;
+    ex.rows = rows;
+    ex.offsets = offsets;
+    ex.n_experts = n_experts;
+    ex.x_rows = T;
+    (void)hipGetLastError();
+    st = from_hip(masq::launch_smooth_quant(x, to_dt(x_dt), modality, inv_smooth, T, c_in, n_mod, w.q,
+                                            w.x_scale, nullptr, 0, s));
+    if (st != MASQ_OK) return st;
+    if (cmc) {
+        st = from_hip(masq::launch_expert_down(x, to_dt(x_dt), modality, inv_smooth, l_down, to_dt(lr_dt),
+                                               n_slots, c_in, rank, n_mod, w.u, ex, s));
+        if (st != MASQ_OK) return st;
+    }
+    return from_hip(masq::launch_gemm_experts(
+        masq::TileGemm{w.q, w.x_scale, static_cast<const int8_t*>(wq), w_scale, n_slots, c_in, c_out,
+                       modality, w.u, nullptr, rank, n_mod, r_up, to_dt(lr_dt), cmc, nullptr, y,
+                       to_dt(y_dt), w4, false, plan, nullptr, nullptr, s},
+        ex));
+}
+
+masq_status masq_combine_experts(const void* d, masq_dtype dt, const int32_t* slots,
+                                 const float* weights, int64_t T, int64_t n_slots, int64_t c_out,
+                                 int32_t top_k, const void* residual, void* y, void* stream) {
+    masq_status st = check_dims(T, 16, c_out, true);
+    if (st != MASQ_OK) return st;
+    if (top_k < 1 || top_k > masq::kRouteMaxK || n_slots < 0 || n_slots > (1LL << 31) - 1)
+        return MASQ_ERR_SHAPE;
+    if (!valid_dt(dt)) return MASQ_ERR_DTYPE;
+    if (T == 0) return MASQ_OK;
+    if ((!d && n_slots > 0) || !slots || !weights || !y) return MASQ_ERR_NULL;
+    const void* ptrs[] = {d, slots, weights, residual, y};
+    for (const void* p : ptrs)
+        if (!aligned16(p)) return MASQ_ERR_ALIGN;
+    (void)hipGetLastError();
+    return from_hip(masq::launch_combine(d, to_dt(dt), slots, weights, T, n_slots, c_out, top_k, residual,
+                                         y, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -322,6 +322,22 @@ hipError_t launch_gemm(const int8_t* q, const float* x_scale, const int8_t* wq,
                        void* y, DT y_dt, hipStream_t s, TilePlan tile, bool w4 = false,
                        bool a_pair = false);
 
+// Activations of the epilogue (masq_act without its gating bit).
+constexpr int kActNone = 0, kActSilu = 1, kActGelu = 2, kActGeluTanh = 3;
+
+// What a GEMM with an epilogue does past the layer's own result, and, for the
+// experts' layer, where its rows and their experts are.
+struct TileExtra {
+    const float* bias;        // [N] (experts: [n_experts][N]) or null
+    const void* residual;     // [T][outputs] in y's type, or null; may be y
+    int act;                  // kAct*
+    bool gated;               // channels 2 i and 2 i + 1: gate and up of output i
+    const int32_t* rows;      // [slots]: the row of x behind a slot; null: the slot's own index
+    const int32_t* offsets;   // [n_experts + 1]: expert e's slots
+    int n_experts;
+    int64_t x_rows;
+};
+
 // The small-tile GEMM; arguments as launch_gemm's.  part / tickets: plan.S
 // slots of bm x bn int32 per tile and an arrival counter (zero on entry, left
 // zero) per tile, for plan.S > 1.
@@ -348,6 +364,8 @@ struct TileGemm {
     hipStream_t stream;
 };
 hipError_t launch_gemm_tile(const TileGemm& g);
+// The same with bias, activation and residual (no accumulator output).
+hipError_t launch_gemm_tile_epilogue(const TileGemm& g, const TileExtra& ex);
 
 // The decode GEMM (small_path): u (null without compensation) holds u_slices
 // partials [T][rank]; part: the decode workspace's [slices + 1][kSmallMaxT][N],
@@ -372,6 +390,38 @@ struct StreamGemm {
     hipStream_t stream;
 };
 hipError_t launch_gemm_stream(const StreamGemm& g);
+hipError_t launch_gemm_stream_epilogue(const StreamGemm& g, const TileExtra& ex);
+
+// The layer over rows sorted by expert (n_slots = g.T output rows; g.mod,
+// g.x_scale and g.q by row of x, g.u by slot; plain codes, one slice).
+// expert_tiles: the most tiles of bm rows that the slots can make, whatever
+// their distribution.
+inline int64_t expert_tiles(int64_t n_slots, int64_t n_experts, int64_t bm) {
+    return n_slots / bm + (n_slots < n_experts ? n_slots : n_experts);
+}
+hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex);
+hipError_t launch_expert_down(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
+                              const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
+                              int n_mod, float* u, const TileExtra& ex, hipStream_t s);
+
+// Routing: at most kRouteMaxExperts experts and kRouteMaxK choices a token.
+// blocks == 0: one workgroup takes the batch and no workspace is needed.
+constexpr int kRouteMaxExperts = 512, kRouteMaxK = 16;
+struct RouteWs {
+    int64_t blocks;
+    uint32_t* masks;      // [blocks][n_experts]
+    int32_t* before;      // [blocks][n_experts]
+    int32_t* totals;      // [n_experts]
+    size_t bytes;
+};
+RouteWs plan_route(void* base, int64_t T, int E);
+hipError_t launch_route(const void* logits, DT dt, const int32_t* mod, int64_t T, int E, int k,
+                        bool renorm, int32_t* experts, float* weights, int32_t* offsets,
+                        int32_t* rows, int32_t* slots, int32_t* slot_mod, const RouteWs& w,
+                        hipStream_t s);
+hipError_t launch_combine(const void* d, DT dt, const int32_t* slots, const float* weights, int64_t T,
+                          int64_t n_slots, int64_t N, int k, const void* residual, void* y,
+                          hipStream_t s);
 
 // MAS-only comparator (a weight per modality, no compensation): rows grouped
 // by modality on the device, then the direct-to-LDS GEMM over tiles of one

@@ -1,0 +1,612 @@
+// The operators around the quantised layer of a decoder block.
+//
+//   layer epilogue   the layer's GEMMs (masq_tile.h) with bias, activation and
+//                    residual: launch_gemm_tile_epilogue, launch_gemm_stream_epilogue
+//   k_route_*        the k largest logits of a token, their softmax weights, and
+//                    the choices of all tokens sorted by expert
+//   k_expert_down    u = (x S^-1) L1 of an expert's rows
+//   k_gemm_tile      (kTileExperts) the layer over rows sorted by expert
+//   k_combine        a token's expert rows, weighted and summed
+
+#include "masq_tile.h"
+
+namespace masq {
+namespace {
+
+// ================================================================ layer epilogue
+template <typename YT, typename LT, bool CMC, bool W4, int MODE>
+hipError_t launch_tile_mode(const TileGemm& g, const TileExtra& ex, int tiles_m) {
+    const int bn = kTileShapes[g.plan.shape].bn;
+    const int tiles_n = static_cast<int>((g.N + bn - 1) / bn);
+    const int64_t nt = static_cast<int64_t>(tiles_m) * tiles_n * g.plan.S;
+#define MASQ_TILE(BM, BN, WM, WN, NST, WPE)                                                         \
+    hipLaunchKernelGGL((k_gemm_tile<YT, LT, CMC, false, W4, BM, BN, WM, WN, NST, WPE, MODE>),       \
+                       grid_of(8 * ((nt + 7) / 8), 64 * WM * WN), dim3(64 * WM * WN), 0, g.stream,  \
+                       g.q, g.wq, g.x_scale, g.w_scale, g.T, static_cast<int>(g.K),                 \
+                       static_cast<int>(g.N), tiles_m, tiles_n, g.mod, g.u, g.u_hl, g.rank,         \
+                       g.n_mod, static_cast<const LT*>(g.r_up), nullptr, static_cast<YT*>(g.y),     \
+                       g.plan.S, g.part, g.tickets, g.a_pair, ex)
+    switch (g.plan.shape) {
+        case 0: MASQ_TILE(32, 64, 1, 2, 3, 2); break;
+        case 1: MASQ_TILE(64, 64, 2, 2, 3, 3); break;
+        case 2: MASQ_TILE(128, 128, 2, 2, 2, 2); break;
+        default: return hipErrorInvalidValue;
+    }
+#undef MASQ_TILE
+    return hipGetLastError();
+}
+
+template <int MODE>
+hipError_t launch_tile_any(const TileGemm& g, const TileExtra& ex, int tiles_m) {
+#define MASQ_MODE(YT, LT, CMC)                                                                      \
+    (g.w4 ? launch_tile_mode<YT, LT, CMC, true, MODE>(g, ex, tiles_m)                               \
+          : launch_tile_mode<YT, LT, CMC, false, MODE>(g, ex, tiles_m))
+    if (!g.cmc) return g.y_dt == DT::BF16 ? MASQ_MODE(bf16_t, bf16_t, false) : MASQ_MODE(float, bf16_t, false);
+    if (g.y_dt == DT::BF16)
+        return g.lr_dt == DT::BF16 ? MASQ_MODE(bf16_t, bf16_t, true) : MASQ_MODE(bf16_t, float, true);
+    return g.lr_dt == DT::BF16 ? MASQ_MODE(float, bf16_t, true) : MASQ_MODE(float, float, true);
+#undef MASQ_MODE
+}
+
+template <typename YT, typename LT, bool W4>
+hipError_t launch_stream_epi(const StreamGemm& g, const TileExtra& ex) {
+    int ns = 0, sp = 0, groups = 0;
+    plan_decode(g.K, g.N, ns, sp, groups);
+    const int S = stream_slices(g.K, groups, ns);
+    const size_t lds = g.u != nullptr ? static_cast<size_t>((g.T + S - 1) / S) * g.rank * sizeof(float)
+                                      : 0;
+    hipLaunchKernelGGL((k_gemm_stream<YT, LT, W4, kTileEpilogue>), dim3(static_cast<unsigned>(groups * S)),
+                       dim3(kStrThreads), lds, g.stream, g.q, g.wq, g.x_scale, g.w_scale,
+                       static_cast<int>(g.T), static_cast<int>(g.K), static_cast<int>(g.N), S, g.mod, g.u,
+                       g.u_slices, g.rank, g.n_mod, static_cast<const LT*>(g.r_up), g.part, g.tickets,
+                       static_cast<YT*>(g.y), -1, ex);
+    return hipGetLastError();
+}
+
+// ================================================================ routing
+// A token's experts: a wave holds its logits, lane l those of experts l, l +
+// 64, ..., as unsigned keys in the order of the values (0: -inf and NaN, never
+// chosen; -0 and +0 alike).  Each of the k rounds takes the largest key of the
+// wave (a chain of lane shifts) and its first holder (a ballot per 64 experts),
+// so ties go to the lowest index.
+//
+// The choices of 32 tokens leave a bit mask per expert (bit t: token t of the
+// block chose it; a token never chooses one twice), which is all that sorting
+// by expert needs: the count of the block is its population count, and a
+// choice's place among the block's the count of the bits below its own.  So
+// slots ascend with the token inside an expert, whatever order anything ran in.
+constexpr int kRouteTokens = 32;
+constexpr int kRouteOneTokens = 256;      // at most this many: one workgroup does it all
+constexpr int kRouteOneThreads = 1024;
+
+__device__ __forceinline__ uint32_t logit_key(float f) {
+    if (!(f > -INFINITY)) return 0;                          // -inf, NaN
+    const uint32_t b = __float_as_uint(f + 0.f);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_logit(uint32_t k) {
+    return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+
+// The largest of the lanes' values, in every lane: lane shifts within rows of
+// 16, then the rows' last lanes onto the rows behind them.
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+#define MASQ_DPP_MAX(ctrl, rows)                                                                    \
+    v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), ctrl, rows, 0xf, false)))
+    MASQ_DPP_MAX(0x111, 0xf);                                // row_shr:1
+    MASQ_DPP_MAX(0x112, 0xf);
+    MASQ_DPP_MAX(0x114, 0xf);
+    MASQ_DPP_MAX(0x118, 0xf);
+    MASQ_DPP_MAX(0x142, 0xa);                                // row_bcast:15
+    MASQ_DPP_MAX(0x143, 0xc);                                // row_bcast:31
+#undef MASQ_DPP_MAX
+    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// Token t's choices by one wave: experts and weights to global memory, the
+// experts' mask bits to masks[expert].
+template <typename LT, int C>
+__device__ __forceinline__ void route_token(const LT* __restrict__ logits, int64_t t, int E, int k,
+                                            bool renorm, int32_t* __restrict__ experts,
+                                            float* __restrict__ weights, uint32_t* masks, int bit,
+                                            int lane) {
+    uint32_t key[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int e = lane + 64 * c;
+        const float f = Elem<LT>::load1(logits + t * E + min(e, E - 1));
+        key[c] = e < E ? logit_key(f) : 0;
+    }
+    uint32_t all[C];                                         // as read (the rounds clear the chosen)
+#pragma unroll
+    for (int c = 0; c < C; ++c) all[c] = key[c];
+    uint32_t top = 0, mine = 0;
+    int pick = -1;                                           // lane j: choice j
+    for (int j = 0; j < k; ++j) {
+        uint32_t best = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) best = max(best, key[c]);
+        best = wave_umax(best);
+        if (best == 0) break;                                // uniform: nothing left
+        if (j == 0) top = best;
+        int e = -1;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const unsigned long long has = __ballot(key[c] == best);
+            if (e < 0 && has != 0) {                         // uniform
+                const int l = __builtin_ctzll(has);
+                e = 64 * c + l;
+                if (lane == l) key[c] = 0;
+            }
+        }
+        if (lane == j) {
+            pick = e;
+            mine = best;
+        }
+    }
+    const float hi = key_logit(top);
+    auto prob = [&](uint32_t q) __attribute__((always_inline)) {
+        return q == 0 ? 0.f : (q == top ? 1.f : expf(key_logit(q) - hi));
+    };
+    const float p = prob(mine);
+    float part = p;
+    if (!renorm) {
+        part = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) part += prob(all[c]);
+    }
+    const float total = wave_sum(part);
+    if (lane < k) {
+        experts[t * k + lane] = pick;
+        weights[t * k + lane] = pick >= 0 ? p / total : 0.f;
+        if (pick >= 0) atomicOr(&masks[pick], 1u << bit);
+    }
+}
+
+template <typename LT>
+__device__ __forceinline__ void route_token_any(const LT* logits, int64_t t, int E, int k, bool renorm,
+                                                int32_t* experts, float* weights, uint32_t* masks,
+                                                int bit, int lane) {
+    if (E <= 64) route_token<LT, 1>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
+    else if (E <= 128) route_token<LT, 2>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
+    else if (E <= 256) route_token<LT, 4>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
+    else route_token<LT, 8>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
+}
+
+// Exclusive prefix of v over the workgroup's first kRouteMaxExperts threads
+// (all NT threads call; the others give 0); *total: the sum.
+template <int NT>
+__device__ __forceinline__ int expert_prefix(int v, int* waves, int* total, int tid) {
+    const int lane = tid & 63, wave = tid >> 6;
+    int s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int p = __shfl_up(s, o);
+        s += lane >= o ? p : 0;
+    }
+    if (lane == 63) waves[wave] = s;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        const int x = waves[w];
+        before += w < wave ? x : 0;
+        all += x;
+    }
+    *total = all;
+    return before + s - v;
+}
+
+// One workgroup for the whole batch (at most kRouteOneTokens tokens).
+template <typename LT>
+__global__ __launch_bounds__(kRouteOneThreads) void k_route_one(
+    const LT* __restrict__ logits, const int32_t* __restrict__ mod, int T, int E, int k, bool renorm,
+    int32_t* __restrict__ experts, float* __restrict__ weights, int32_t* __restrict__ offsets,
+    int32_t* __restrict__ rows, int32_t* __restrict__ slots, int32_t* __restrict__ slot_mod) {
+    constexpr int kWords = kRouteOneTokens / 32, NW = kRouteOneThreads / 64;
+    __shared__ uint32_t masks[kWords][kRouteMaxExperts];
+    __shared__ int base[kRouteMaxExperts];
+    __shared__ int waves[NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int words = (T + 31) >> 5;
+    for (int i = tid; i < words * kRouteMaxExperts; i += kRouteOneThreads) (&masks[0][0])[i] = 0;
+    __syncthreads();
+    for (int t = wave; t < T; t += NW)                       // wave-uniform
+        route_token_any<LT>(logits, t, E, k, renorm, experts, weights, masks[t >> 5], t & 31, lane);
+    __syncthreads();
+    int cnt = 0, total;
+    if (tid < E)
+        for (int w = 0; w < words; ++w) cnt += __popc(masks[w][tid]);
+    const int first = expert_prefix<kRouteOneThreads>(cnt, waves, &total, tid);
+    if (tid < E) {
+        base[tid] = first;
+        offsets[tid] = first;
+    }
+    if (tid == 0) offsets[E] = total;
+    __syncthreads();
+    for (int i = tid; i < T * k; i += kRouteOneThreads) {
+        const int t = i / k;
+        const int e = experts[i];                            // written by this workgroup before the barrier
+        int slot = -1;
+        if (e >= 0) {
+            slot = base[e] + __popc(masks[t >> 5][e] & ((1u << (t & 31)) - 1u));
+            for (int w = 0; w < (t >> 5); ++w) slot += __popc(masks[w][e]);
+            rows[slot] = t;
+            if (slot_mod != nullptr) slot_mod[slot] = mod[t];
+        }
+        slots[i] = slot;
+        if (i >= total) {                                    // past the last choice
+            rows[i] = -1;
+            if (slot_mod != nullptr) slot_mod[i] = 0;
+        }
+    }
+}
+
+// Larger batches, in three launches: the choices and the masks of every 32
+// tokens, the masks' counts summed over the blocks before each, the places.
+template <typename LT>
+__global__ __launch_bounds__(256) void k_route_choose(
+    const LT* __restrict__ logits, int64_t T, int E, int k, bool renorm, int32_t* __restrict__ experts,
+    float* __restrict__ weights, uint32_t* __restrict__ masks) {
+    __shared__ uint32_t sm[kRouteMaxExperts];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int e = tid; e < E; e += 256) sm[e] = 0;
+    __syncthreads();
+    const int64_t t0 = linear_block() * kRouteTokens;
+    if (t0 >= T) return;
+    for (int i = wave; i < kRouteTokens && t0 + i < T; i += 4)
+        route_token_any<LT>(logits, t0 + i, E, k, renorm, experts, weights, sm, i, lane);
+    __syncthreads();
+    for (int e = tid; e < E; e += 256) masks[linear_block() * E + e] = sm[e];
+}
+
+// A workgroup per 16 experts: 64 thread rows, each over a run of blocks.
+constexpr int kScanCols = 16, kScanRows = 64;
+__global__ __launch_bounds__(kScanCols * kScanRows) void k_route_scan(
+    const uint32_t* __restrict__ masks, int64_t blocks, int E, int32_t* __restrict__ before,
+    int32_t* __restrict__ totals) {
+    __shared__ int part[kScanRows][kScanCols];
+    const int col = threadIdx.x % kScanCols, row = threadIdx.x / kScanCols;
+    const int e = blockIdx.x * kScanCols + col;
+    const bool in = e < E;
+    const int64_t per = (blocks + kScanRows - 1) / kScanRows;
+    const int64_t b0 = min(blocks, row * per), b1 = min(blocks, b0 + per);
+    int sum = 0;
+    if (in)
+        for (int64_t b = b0; b < b1; ++b) sum += __popc(masks[b * E + e]);
+    part[row][col] = sum;
+    __syncthreads();
+    int at = 0, all = 0;
+    for (int r = 0; r < kScanRows; ++r) {
+        const int x = part[r][col];
+        at += r < row ? x : 0;
+        all += x;
+    }
+    if (!in) return;
+    for (int64_t b = b0; b < b1; ++b) {
+        before[b * E + e] = at;
+        at += __popc(masks[b * E + e]);
+    }
+    if (row == 0) totals[e] = all;
+}
+
+__global__ __launch_bounds__(kRouteMaxExperts) void k_route_place(
+    const int32_t* __restrict__ mod, int64_t T, int E, int k, const int32_t* __restrict__ experts,
+    const uint32_t* __restrict__ masks, const int32_t* __restrict__ before,
+    const int32_t* __restrict__ totals, int32_t* __restrict__ offsets, int32_t* __restrict__ rows,
+    int32_t* __restrict__ slots, int32_t* __restrict__ slot_mod) {
+    constexpr int NT = kRouteMaxExperts;
+    __shared__ int base[NT];
+    __shared__ uint32_t sm[NT];
+    __shared__ int waves[NT / 64];
+    const int tid = threadIdx.x;
+    const int64_t b = linear_block(), t0 = b * kRouteTokens;
+    if (t0 >= T) return;
+    int total;
+    const int first = expert_prefix<NT>(tid < E ? totals[tid] : 0, waves, &total, tid);
+    if (tid < E) {
+        base[tid] = first + before[b * E + tid];
+        sm[tid] = masks[b * E + tid];
+        if (b == 0) offsets[tid] = first;
+    }
+    if (b == 0 && tid == 0) offsets[E] = total;
+    __syncthreads();
+    const int n = static_cast<int>(min(T - t0, static_cast<int64_t>(kRouteTokens))) * k;
+    for (int i = tid; i < n; i += NT) {
+        const int t = i / k;
+        const int e = experts[t0 * k + i];
+        int slot = -1;
+        if (e >= 0) {
+            slot = base[e] + __popc(sm[e] & ((1u << t) - 1u));
+            rows[slot] = static_cast<int32_t>(t0 + t);
+            if (slot_mod != nullptr) slot_mod[slot] = mod[t0 + t];
+        }
+        slots[t0 * k + i] = slot;
+        if (t0 * k + i >= total) {                           // past the last choice
+            rows[t0 * k + i] = -1;
+            if (slot_mod != nullptr) slot_mod[t0 * k + i] = 0;
+        }
+    }
+}
+
+// ================================================================ experts' down-projection
+// u[slot] = (x S_m^-1) L1_e^m for the slots of modality m != text: a workgroup
+// takes 32 slots of one expert and 64 columns of the rank, its eight waves an
+// eighth of the row each, and the waves' sums are added in their order.  With
+// bf16 factors the smoothed row enters as a hi + lo pair of bf16 terms, as in
+// the layer; with fp32 factors the fp32 MFMA takes it whole.  Each modality is
+// summed on its own, so that an infinite factor stays with its modality.
+constexpr int kEdSlots = 32, kEdWaves = 8, kEdRank = 64;
+
+template <typename XT, typename LT>
+__global__ __launch_bounds__(64 * kEdWaves) void k_expert_down(
+    const XT* __restrict__ x, const int32_t* __restrict__ mod, const float* __restrict__ inv_s,
+    const LT* __restrict__ l_down, int64_t n_slots, int K, int r, int n_mod, float* __restrict__ u,
+    TileExtra ex) {
+    constexpr int RG = kEdSlots / 16, RB = kEdRank / 16;
+    static_assert(RG * RB * 64 == 64 * kEdWaves, "a thread finishes one 16-byte piece of u");
+    __shared__ __attribute__((aligned(16))) v4f red[kEdWaves][RG * RB * 64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    GroupTile gt;
+    if (!group_tile<kEdSlots>(ex, n_slots, linear_block(), (r + kEdRank - 1) / kEdRank, gt)) return;
+    const int c0 = gt.tn * kEdRank;
+    const int nb = min(RB, (r - c0) >> 4);                   // 16-column blocks of the rank
+    const int steps = (K + 31) >> 5, per = (steps + kEdWaves - 1) / kEdWaves;
+    const int st0 = wave * per, st1 = min(steps, st0 + per);
+    const XT* xp[RG];
+    const float* ip[RG];
+    int md[RG];
+#pragma unroll
+    for (int g = 0; g < RG; ++g) {
+        const int64_t ar = slot_row(ex, min(gt.first + 16 * g + (lane & 15), gt.end - 1));
+        md[g] = sane_mod(mod[ar], n_mod);
+        xp[g] = x + ar * K;
+        ip[g] = inv_s + static_cast<int64_t>(md[g]) * K;
+    }
+    for (int m = 1; m < n_mod; ++m) {
+        bool live[RG], any = false;
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            live[g] = md[g] == m;
+            any = any || live[g];
+        }
+        if (__ballot(any) == 0ull) continue;                 // uniform over the workgroup: same rows
+        const LT* lm = l_down + (static_cast<int64_t>(gt.expert) * (n_mod - 1) + m - 1) * r * K;
+        v4f acc[RG][RB];
+#pragma unroll
+        for (int g = 0; g < RG; ++g)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) acc[g][b] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int st = st0; st < st1; ++st) {
+            const int k = 32 * st + 8 * (lane >> 4);
+            const bool in = k < K;                           // K % 16 == 0: 8 columns in or out together
+            const int kc = min(k, K - 8);
+            Raw8<LT> lv[RB];
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+                lv[b].load(lm + static_cast<int64_t>(c0 + 16 * min(b, nb - 1) + (lane & 15)) * K + kc);
+            float xs[RG][8];
+#pragma unroll
+            for (int g = 0; g < RG; ++g) {
+                float f[8], s[8];
+                Elem<XT>::load8(xp[g] + kc, f);
+                load8_f32(ip[g] + kc, s);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xs[g][e] = live[g] && in ? f[e] * s[e] : 0.f;
+            }
+            if constexpr (sizeof(LT) == 2) {
+                const v4i zero = {0, 0, 0, 0};
+#pragma unroll
+                for (int g = 0; g < RG; ++g) {
+                    v4i hi, lo;
+                    split_bf16x8(xs[g], hi, lo);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        const v8bf w = __builtin_bit_cast(v8bf, in ? lv[b].a : zero);
+                        acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, hi), acc[g][b], 0, 0, 0);
+                        acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, lo), acc[g][b], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                    float w[8];
+                    lv[b].to_f32(w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+#pragma unroll
+                        for (int g = 0; g < RG; ++g)
+                            acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? w[e] : 0.f, xs[g][e], acc[g][b], 0, 0, 0);
+                }
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < RG; ++g)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) red[wave][(g * RB + b) * 64 + lane] = acc[g][b];
+        __syncthreads();
+        // thread tid: block (g, b) = wave, its lane's columns 4 (lane / 16) .. of slot lane % 16
+        v4f v = red[0][tid];
+#pragma unroll
+        for (int w = 1; w < kEdWaves; ++w) v = v + red[w][tid];
+        const int g = wave / RB, b = wave % RB;
+        const int64_t slot = gt.first + 16 * g + (lane & 15);
+        const bool mine = g == 0 ? live[0] : live[RG - 1];
+        if (b < nb && slot < gt.end && mine)
+            *reinterpret_cast<v4f*>(u + slot * r + c0 + 16 * b + 4 * (lane >> 4)) = v;
+        __syncthreads();                                     // red is free for the next modality
+    }
+}
+
+// ================================================================ combination
+// y[t] = residual[t] + sum over j of weights[t][j] d[slots[t][j]], in fp32 in
+// the order of j, rounded once.  8 columns a thread; a token's rows are read
+// together (KMAX loads in flight).  A slot outside [0, n_slots) adds nothing.
+template <typename DTy, int KB>
+__global__ __launch_bounds__(256) void k_combine(const DTy* __restrict__ d,
+                                                 const int32_t* __restrict__ slots,
+                                                 const float* __restrict__ weights, int64_t T,
+                                                 int64_t n_slots, int N, int k,
+                                                 const DTy* residual, DTy* y) {
+    const int per_row = N >> 3;
+    const int64_t i = linear_block() * 256 + threadIdx.x;
+    if (i >= T * per_row) return;
+    const int64_t t = i / per_row;
+    const int o = static_cast<int>(i - t * per_row) * 8;
+    float v[8] = {};
+    for (int j0 = 0; j0 < k; j0 += KB) {
+        Raw8<DTy> raw[KB];
+        float w[KB];
+        bool in[KB];
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+            const int64_t at = t * k + min(j0 + j, k - 1);
+            const int64_t s = slots[at];
+            in[j] = j0 + j < k && s >= 0 && s < n_slots;
+            w[j] = weights[at];
+            if (in[j]) raw[j].load(d + s * N + o);
+        }
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+            if (!in[j]) continue;
+            float f[8];
+            raw[j].to_f32(f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(w[j], f[e], v[e]);
+        }
+    }
+    if (residual != nullptr) {
+        float q[8];
+        Elem<DTy>::load8(residual + t * N + o, q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += q[e];
+    }
+    DTy* dst = y + t * N + o;
+    if constexpr (sizeof(DTy) == 2) {
+        *reinterpret_cast<v4i*>(dst) =
+            v4i{static_cast<int32_t>(pack_bf16x2(v[0], v[1])), static_cast<int32_t>(pack_bf16x2(v[2], v[3])),
+                static_cast<int32_t>(pack_bf16x2(v[4], v[5])), static_cast<int32_t>(pack_bf16x2(v[6], v[7]))};
+    } else {
+        *reinterpret_cast<v4f*>(dst) = v4f{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<v4f*>(dst + 4) = v4f{v[4], v[5], v[6], v[7]};
+    }
+}
+
+}  // namespace
+
+// ================================================================ launchers
+hipError_t launch_gemm_tile_epilogue(const TileGemm& g, const TileExtra& ex) {
+    if (g.K % 16 != 0 || g.N % (ex.gated ? 32 : 16) != 0 || g.plan.S < 1 || (g.w4 && g.K % 64 != 0) ||
+        (g.a_pair && g.K % 64 != 0) || (g.plan.S > 1 && (g.part == nullptr || g.tickets == nullptr)) ||
+        g.plan.shape < 0 || g.acc != nullptr)
+        return hipErrorInvalidValue;
+    const int bm = kTileShapes[g.plan.shape].bm;
+    return launch_tile_any<kTileEpilogue>(g, ex, static_cast<int>((g.T + bm - 1) / bm));
+}
+
+hipError_t launch_gemm_stream_epilogue(const StreamGemm& g, const TileExtra& ex) {
+    if (!small_path(g.T, g.K) || g.N % (ex.gated ? 32 : 16) != 0 || g.part == nullptr ||
+        g.tickets == nullptr || g.only_mod >= 0)
+        return hipErrorInvalidValue;
+#define MASQ_STREAM(YT, LT) (g.w4 ? launch_stream_epi<YT, LT, true>(g, ex) : launch_stream_epi<YT, LT, false>(g, ex))
+    if (g.y_dt == DT::BF16) return g.lr_dt == DT::BF16 ? MASQ_STREAM(bf16_t, bf16_t) : MASQ_STREAM(bf16_t, float);
+    return g.lr_dt == DT::BF16 ? MASQ_STREAM(float, bf16_t) : MASQ_STREAM(float, float);
+#undef MASQ_STREAM
+}
+
+hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex) {
+    if (g.K % 16 != 0 || g.N % (ex.gated ? 32 : 16) != 0 || g.plan.S != 1 || (g.w4 && g.K % 64 != 0) ||
+        g.a_pair || g.plan.shape < 0 || g.acc != nullptr || g.u_hl != nullptr)
+        return hipErrorInvalidValue;
+    return launch_tile_any<kTileExperts>(
+        g, ex, static_cast<int>(expert_tiles(g.T, ex.n_experts, kTileShapes[g.plan.shape].bm)));
+}
+
+hipError_t launch_expert_down(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
+                              const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
+                              int n_mod, float* u, const TileExtra& ex, hipStream_t s) {
+    const int64_t nt = expert_tiles(n_slots, ex.n_experts, kEdSlots) * ((rank + kEdRank - 1) / kEdRank);
+    const dim3 grid = grid_of(8 * ((nt + 7) / 8), 64 * kEdWaves), block(64 * kEdWaves);
+#define MASQ_DOWN(XT, LT)                                                                           \
+    hipLaunchKernelGGL((k_expert_down<XT, LT>), grid, block, 0, s, static_cast<const XT*>(x), mod,  \
+                       inv_s, static_cast<const LT*>(l_down), n_slots, static_cast<int>(K), rank,   \
+                       n_mod, u, ex)
+    if (x_dt == DT::BF16) {
+        if (lr_dt == DT::BF16) MASQ_DOWN(bf16_t, bf16_t);
+        else MASQ_DOWN(bf16_t, float);
+    } else {
+        if (lr_dt == DT::BF16) MASQ_DOWN(float, bf16_t);
+        else MASQ_DOWN(float, float);
+    }
+#undef MASQ_DOWN
+    return hipGetLastError();
+}
+
+hipError_t launch_route(const void* logits, DT dt, const int32_t* mod, int64_t T, int E, int k,
+                        bool renorm, int32_t* experts, float* weights, int32_t* offsets,
+                        int32_t* rows, int32_t* slots, int32_t* slot_mod, const RouteWs& w,
+                        hipStream_t s) {
+    if (w.blocks == 0) {                                     // plan_route: one workgroup
+#define MASQ_ROUTE(LT)                                                                              \
+    hipLaunchKernelGGL(k_route_one<LT>, dim3(1), dim3(kRouteOneThreads), 0, s,                      \
+                       static_cast<const LT*>(logits), mod, static_cast<int>(T), E, k, renorm,      \
+                       experts, weights, offsets, rows, slots, slot_mod)
+        if (dt == DT::BF16) MASQ_ROUTE(bf16_t);
+        else MASQ_ROUTE(float);
+#undef MASQ_ROUTE
+        return hipGetLastError();
+    }
+    const dim3 grid = grid_of(w.blocks, 256);
+#define MASQ_ROUTE(LT)                                                                              \
+    hipLaunchKernelGGL(k_route_choose<LT>, grid, dim3(256), 0, s, static_cast<const LT*>(logits),   \
+                       T, E, k, renorm, experts, weights, w.masks)
+    if (dt == DT::BF16) MASQ_ROUTE(bf16_t);
+    else MASQ_ROUTE(float);
+#undef MASQ_ROUTE
+    hipLaunchKernelGGL(k_route_scan, dim3(static_cast<unsigned>((E + kScanCols - 1) / kScanCols)),
+                       dim3(kScanCols * kScanRows), 0, s, w.masks, w.blocks, E, w.before, w.totals);
+    hipLaunchKernelGGL(k_route_place, grid_of(w.blocks, kRouteMaxExperts), dim3(kRouteMaxExperts), 0, s,
+                       mod, T, E, k, experts, w.masks, w.before, w.totals, offsets, rows, slots, slot_mod);
+    return hipGetLastError();
+}
+
+RouteWs plan_route(void* base, int64_t T, int E) {
+    RouteWs w{};
+    if (T <= kRouteOneTokens) return w;
+    w.blocks = (T + kRouteTokens - 1) / kRouteTokens;
+    const size_t table = (static_cast<size_t>(w.blocks) * E * 4 + 255) / 256 * 256;
+    uint8_t* b = static_cast<uint8_t*>(base);
+    if (b != nullptr) {
+        w.masks = reinterpret_cast<uint32_t*>(b);
+        w.before = reinterpret_cast<int32_t*>(b + table);
+        w.totals = reinterpret_cast<int32_t*>(b + 2 * table);
+    }
+    w.bytes = 2 * table + (static_cast<size_t>(E) * 4 + 255) / 256 * 256;
+    return w;
+}
+
+hipError_t launch_combine(const void* d, DT dt, const int32_t* slots, const float* weights, int64_t T,
+                          int64_t n_slots, int64_t N, int k, const void* residual, void* y,
+                          hipStream_t s) {
+    const dim3 grid = grid_of((T * (N / 8) + 255) / 256, 256);
+#define MASQ_COMBINE(DTy, KB)                                                                       \
+    hipLaunchKernelGGL((k_combine<DTy, KB>), grid, dim3(256), 0, s, static_cast<const DTy*>(d), slots, \
+                       weights, T, n_slots, static_cast<int>(N), k,                                 \
+                       static_cast<const DTy*>(residual), static_cast<DTy*>(y))
+    if (dt == DT::BF16) {
+        if (k > 4) MASQ_COMBINE(bf16_t, 8);
+        else MASQ_COMBINE(bf16_t, 4);
+    } else {
+        MASQ_COMBINE(float, 4);
+    }
+#undef MASQ_COMBINE
+    return hipGetLastError();
+}
+
+}  // namespace masq

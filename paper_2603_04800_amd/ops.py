@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import typing
 
 import torch
 
@@ -49,6 +50,15 @@ _SIGS = {
     "masq_linear_fused_w4a8": (_FUSED_ARGS, ctypes.c_int),
     "masq_linear_stage1_w4a8": (_FUSED_ARGS, ctypes.c_int),
     "masq_linear_stage2_w4a8": (_FUSED_ARGS, ctypes.c_int),
+    "masq_linear_epilogue": ([_p, _i32, _p, _p, _p, _i32, _p, _p, _p, _i32, _i64, _i64, _i64, _i32,
+                              _i32, _p, _i32, _p, _p, _i32, _p, _sz, _p], ctypes.c_int),
+    "masq_route_experts": ([_p, _i32, _p, _i64, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _sz,
+                            _p], ctypes.c_int),
+    "masq_route_experts_workspace_bytes": ([_i64, _i32], ctypes.c_size_t),
+    "masq_expert_linear": ([_p, _i32, _i64, _p, _p, _p, _i32, _p, _p, _p, _i32, _p, _p, _i64, _i32,
+                            _i64, _i64, _i32, _i32, _p, _i32, _p, _i32, _p, _sz, _p], ctypes.c_int),
+    "masq_expert_linear_workspace_bytes": ([_i64, _i64, _i64, _i32, _i32], ctypes.c_size_t),
+    "masq_combine_experts": ([_p, _i32, _p, _p, _i64, _i64, _i64, _i32, _p, _p, _p], ctypes.c_int),
     "masq_channel_range": ([_p, _i32, _p, _i64, _i64, _i32, _p, _p], ctypes.c_int),
     "masq_smoothing_factors": ([_p, _p, _i64, _i64, _i32, _p, _p, _p], ctypes.c_int),
     "masq_quantize_weight": ([_p, _p, _i64, _i64, _i32, _p, _p, _p], ctypes.c_int),
@@ -395,6 +405,149 @@ def mas_gradient(x, a, w, b, smooth, stream=None):
     return grad
 
 
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
+_GATED = 16
+
+
+def _act(act, gated) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {act!r} (one of {', '.join(ACTIVATIONS)})")
+    return ACTIVATIONS[act] + (_GATED if gated else 0)
+
+
+def _shaped(t, shape, dtype, name):
+    """Check an optional tensor's type and shape."""
+    if t is None:
+        return
+    _need(t, dtype, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _device_of(**tensors):
+    """The one device that all the tensors given live on."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must live on the GPU")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, other tensors on {dev}")
+        dev = t.device
+    return dev
+
+
+def _empty(shape, dtype, dev, stream):
+    """Memory of the stream that the call will run on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _on(dev, stream):
+    """The call's stream: the one given, else dev's current one."""
+    s = stream if stream is not None else torch.cuda.current_stream(dev)
+    if s.device != dev:
+        raise ValueError(f"the stream is on {s.device}, the tensors on {dev}")
+    return ctypes.c_void_p(s.cuda_stream)
+
+
+class BoundCall:
+    """One C call on fixed buffers with its arguments checked and converted
+    once: calling it enqueues the work on the stream it was bound to and
+    returns `result`, the tensors it writes.  Keeps its tensors alive, its
+    workspace among them, so calls bound apart may run at the same time."""
+
+    def __init__(self, name, args, result, dev, keep):
+        self._name, self._fn, self._args = name, getattr(_lib, name), args
+        self.result, self._dev, self._keep = result, dev.index, keep
+
+    def __call__(self):
+        if torch.cuda.current_device() != self._dev:
+            with torch.cuda.device(self._dev):
+                _check(self._name, self._fn(*self._args))
+        else:
+            _check(self._name, self._fn(*self._args))
+        return self.result
+
+
+class Routing(typing.NamedTuple):
+    """What route_experts gives: experts, weights and slots [T][top_k], offsets
+    [n_experts + 1], rows and modality [T top_k] (see masq_route_experts)."""
+    experts: torch.Tensor
+    weights: torch.Tensor
+    offsets: torch.Tensor
+    rows: torch.Tensor
+    slots: torch.Tensor
+    modality: torch.Tensor | None
+
+
+def bind_route_experts(logits, top_k, renormalize=True, modality=None, stream=None):
+    """route_experts on fixed buffers: a BoundCall giving the Routing."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T][n_experts]")
+    T, E = logits.shape
+    dev = _device_of(logits=logits, modality=modality)
+    _shaped(modality, (T,), torch.int32, "modality")
+
+    def new(shape, dtype):
+        return _empty(shape, dtype, dev, stream)
+
+    i32 = torch.int32
+    r = Routing(new((T, top_k), i32), new((T, top_k), torch.float32), new((E + 1,), i32),
+                new((T * top_k,), i32), new((T, top_k), i32),
+                new((T * top_k,), i32) if modality is not None else None)
+    if T == 0:
+        r.offsets.zero_()
+    need = int(_lib.masq_route_experts_workspace_bytes(T, E))
+    ws = new((need,), torch.uint8) if need else None
+    args = (_ptr(logits), _dt(logits), _ptr(modality), T, E, top_k, 1 if renormalize else 0,
+            _ptr(r.experts), _ptr(r.weights), _ptr(r.offsets), _ptr(r.rows), _ptr(r.slots),
+            _ptr(r.modality), _ptr(ws), need, _on(dev, stream))
+    return BoundCall("masq_route_experts", args, r, dev, (logits, modality, ws))
+
+
+def route_experts(logits, top_k, renormalize=True, modality=None, stream=None) -> Routing:
+    """Every token's top_k experts with their softmax weights, and the choices
+    of all tokens sorted by expert.  With modality [T], also each slot's."""
+    return bind_route_experts(logits, top_k, renormalize, modality, stream)()
+
+
+def bind_combine_experts(d, slots, weights, residual=None, out=None, stream=None):
+    """combine_experts on fixed buffers: a BoundCall giving y."""
+    if d.dim() != 2 or slots.dim() != 2:
+        raise ValueError("d must be [n_slots][c_out] and slots [T][top_k]")
+    n, N = d.shape
+    T, k = slots.shape
+    dev = _device_of(d=d, slots=slots, weights=weights, residual=residual, out=out)
+    _need(slots, torch.int32, "slots")
+    _shaped(weights, (T, k), torch.float32, "weights")
+    _shaped(residual, (T, N), d.dtype, "residual")
+    if out is None:
+        out = _empty((T, N), d.dtype, dev, stream)
+    _shaped(out, (T, N), d.dtype, "out")
+    args = (_ptr(d), _dt(d), _ptr(slots), _ptr(weights), T, n, N, k, _ptr(residual), _ptr(out),
+            _on(dev, stream))
+    return BoundCall("masq_combine_experts", args, out, dev, (d, slots, weights, residual))
+
+
+def combine_experts(d, slots, weights, residual=None, out=None, stream=None):
+    """y[t] = residual[t] + sum_j weights[t][j] d[slots[t][j]] (fp32 sums,
+    rounded once); residual may be out."""
+    return bind_combine_experts(d, slots, weights, residual, out, stream)()
+
+
+def interleave_gate_up(gate, up, axis=0):
+    """The channels of a gated layer in pairs: index 2 i of the result along
+    `axis` is gate's i, 2 i + 1 up's (weight rows, scales, r_up rows, biases)."""
+    if gate.shape != up.shape:
+        raise ValueError("gate and up differ in shape")
+    axis = axis % gate.dim()
+    return torch.stack([gate, up], dim=axis + 1).flatten(axis, axis + 1).contiguous()
+
+
 def workspace_bytes(T, K, N, rank, n_mod) -> int:
     return int(_lib.masq_linear_fused_workspace_bytes(T, K, N, rank, n_mod))
 
@@ -482,6 +635,44 @@ class Linear:
         converted once, for tight loops: returns an object whose stage1(),
         stage2() and __call__() each make one C call."""
         return BoundLinear(self, x, modality, out, workspace, stream)
+
+
+    def fused(self, x, modality, bias=None, act="none", gated=False, residual=None, out=None,
+              out_dtype=None, workspace=None, stream=None):
+        """The layer with bias [N] f32, activation and residual in its
+        epilogue (masq_linear_epilogue): act(z + bias) + residual, or, gated
+        (channels 2 i and 2 i + 1: gate and up, see interleave_gate_up),
+        act(z_2i) z_2i+1 + residual of half the width."""
+        return self.bind_fused(x, modality, bias, act, gated, residual, out, out_dtype, workspace,
+                               stream)()
+
+    def bind_fused(self, x, modality, bias=None, act="none", gated=False, residual=None, out=None,
+                   out_dtype=None, workspace=None, stream=None):
+        """fused() on fixed buffers: a BoundCall giving the output."""
+        code = _act(act, gated)
+        if x.dim() != 2 or x.shape[1] != self.c_in:
+            raise ValueError(f"x must be [T][{self.c_in}]")
+        T = x.shape[0]
+        shape = (T, self.c_out // 2 if gated else self.c_out)
+        dev = _device_of(x=x, modality=modality, wq=self.wq, inv_smooth=self.inv_smooth, bias=bias,
+                         residual=residual, out=out, workspace=workspace)
+        _shaped(modality, (T,), torch.int32, "modality")
+        _shaped(bias, (self.c_out,), torch.float32, "bias")
+        if out is None:
+            out = _empty(shape, out_dtype or x.dtype, dev, stream)
+        _shaped(out, shape, out.dtype, "out")
+        _shaped(residual, shape, out.dtype, "residual")
+        ws = workspace
+        if ws is None:
+            need = workspace_bytes(T, self.c_in, self.c_out, self.rank, self.n_mod)
+            ws = _empty((max(need, 256),), torch.uint8, dev, stream)
+        lr_dt = _dt(self.l_down) if self.l_down is not None else F32
+        args = (_ptr(x), _dt(x), _ptr(modality), _ptr(self.inv_smooth), _ptr(self.wq),
+                4 if self.w4 else 8, _ptr(self.w_scale), _ptr(self.l_down), _ptr(self.r_up), lr_dt,
+                T, self.c_in, self.c_out, self.rank, self.n_mod, _ptr(bias), code, _ptr(residual),
+                _ptr(out), _dt(out), _ptr(ws), ws.numel(), _on(dev, stream))
+        return BoundCall("masq_linear_epilogue", args, out, dev,
+                         (self, x, modality, bias, residual, ws))
 
 
 class BoundLinear:
@@ -585,6 +776,98 @@ class BoundMasOnly:
 
     def stage2(self):
         self()
+
+
+class ExpertLinear:
+    """The modality-aware layer of a mixture of experts (masq_expert_linear):
+    rows sorted by expert, each expert with its own weight.
+
+    Holds inv_smooth [M][K] f32 (common to the experts), wq [E][N][K] int8 (or
+    uint8 [E][N][K / 2], packed 4-bit codes), w_scale [E][N] f32, the factors
+    l_down [E][M-1][r][K] and r_up [E][M-1][N][r] (f32 or bf16), bias [E][N]
+    f32, and the activation; gated: channels 2 i and 2 i + 1 are gate and up."""
+
+    def __init__(self, inv_smooth, wq, w_scale, l_down=None, r_up=None, bias=None, act="none",
+                 gated=False):
+        if wq.dim() != 3 or wq.dtype not in (torch.int8, torch.uint8):
+            raise ValueError("wq must be int8 [E][N][K] or packed uint8 [E][N][K / 2]")
+        self.inv_smooth, self.wq, self.w_scale = inv_smooth, wq, w_scale
+        self.l_down, self.r_up, self.bias = l_down, r_up, bias
+        self.w4 = wq.dtype == torch.uint8
+        self.n_experts, self.c_out = wq.shape[:2]
+        self.n_mod, self.c_in = inv_smooth.shape
+        self.act, self.gated, self._act = act, gated, _act(act, gated)
+        if wq.shape[2] * (2 if self.w4 else 1) != self.c_in:
+            raise ValueError("wq does not match inv_smooth's width")
+        self.width = self.c_out // 2 if gated else self.c_out
+        E, M, N = self.n_experts, self.n_mod, self.c_out
+        self.rank = l_down.shape[2] if l_down is not None and l_down.dim() == 4 else 0
+        _need(inv_smooth, torch.float32, "inv_smooth")
+        _shaped(w_scale, (E, N), torch.float32, "w_scale")
+        _shaped(bias, (E, N), torch.float32, "bias")
+        if self.rank:
+            if r_up is None:
+                raise ValueError("l_down needs r_up")
+            _shaped(l_down, (E, M - 1, self.rank, self.c_in), l_down.dtype, "l_down")
+            _shaped(r_up, (E, M - 1, N, self.rank), l_down.dtype, "r_up")
+
+    def bind(self, x, modality, offsets, rows=None, out=None, out_dtype=None, workspace=None,
+             stream=None):
+        """The call on fixed buffers: a BoundCall giving the output."""
+        if x.dim() != 2 or x.shape[1] != self.c_in:
+            raise ValueError(f"x must be [T][{self.c_in}]")
+        T = x.shape[0]
+        n = T if rows is None else rows.numel()
+        dev = _device_of(x=x, modality=modality, offsets=offsets, rows=rows, wq=self.wq,
+                         inv_smooth=self.inv_smooth, out=out, workspace=workspace)
+        _shaped(modality, (T,), torch.int32, "modality")
+        _shaped(offsets, (self.n_experts + 1,), torch.int32, "offsets")
+        _shaped(rows, (n,), torch.int32, "rows")
+        if out is None:
+            out = _empty((n, self.width), out_dtype or x.dtype, dev, stream)
+        _shaped(out, (n, self.width), out.dtype, "out")
+        ws = workspace
+        if ws is None:
+            need = int(_lib.masq_expert_linear_workspace_bytes(T, n, self.c_in, self.rank,
+                                                               self.n_mod))
+            ws = _empty((max(need, 256),), torch.uint8, dev, stream)
+        lr_dt = _dt(self.l_down) if self.l_down is not None else F32
+        args = (_ptr(x), _dt(x), T, _ptr(modality), _ptr(self.inv_smooth), _ptr(self.wq),
+                4 if self.w4 else 8, _ptr(self.w_scale), _ptr(self.l_down), _ptr(self.r_up), lr_dt,
+                _ptr(rows), _ptr(offsets), n, self.n_experts, self.c_in, self.c_out, self.rank,
+                self.n_mod, _ptr(self.bias), self._act, _ptr(out), _dt(out), _ptr(ws), ws.numel(),
+                _on(dev, stream))
+        return BoundCall("masq_expert_linear", args, out, dev,
+                         (self, x, modality, offsets, rows, ws))
+
+    def __call__(self, x, modality, offsets, rows=None, out=None, out_dtype=None, workspace=None,
+                 stream=None):
+        """Rows [n_slots][N] (or N / 2 where gated) by slot.  x [T][K] with the
+        modality of its rows; rows [n_slots]: the row of x of each slot (None:
+        x is in slot order); offsets [E + 1]: the experts' slots.  Rows past
+        offsets[E] are not written."""
+        return self.bind(x, modality, offsets, rows, out, out_dtype, workspace, stream)()
+
+
+class ExpertMLP:
+    """The mixture-of-experts block of a decoder layer on the quantised layers:
+    routing, the gated gate/up layer, the down layer, the combination.
+
+    gate_up: an ExpertLinear K -> 2 I, gated; down: one I -> N."""
+
+    def __init__(self, gate_up, down, top_k, renormalize=True):
+        if gate_up.n_experts != down.n_experts or gate_up.width != down.c_in:
+            raise ValueError("gate_up and down do not fit together")
+        self.gate_up, self.down, self.top_k, self.renormalize = gate_up, down, top_k, renormalize
+
+    def __call__(self, x, modality, logits, residual=None, out=None, stream=None):
+        """x [T][K], modality [T], logits [T][E] -> y [T][N] (+ residual)."""
+        if logits.dim() != 2 or logits.shape != (x.shape[0], self.gate_up.n_experts):
+            raise ValueError(f"logits must be [{x.shape[0]}][{self.gate_up.n_experts}]")
+        r = route_experts(logits, self.top_k, self.renormalize, modality, stream)
+        h = self.gate_up(x, modality, r.offsets, rows=r.rows, stream=stream)
+        d = self.down(h, r.modality, r.offsets, stream=stream)
+        return combine_experts(d, r.slots, r.weights, residual, out, stream)
 
 
 def linear_fused(x, modality, inv_smooth, wq, w_scale, l_down=None, r_up=None,
