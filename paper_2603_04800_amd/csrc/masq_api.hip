@@ -277,11 +277,12 @@ MasOnlyWs plan_mas_only(void* base, int64_t T, int64_t K, int64_t N, int n_mod) 
 }
 
 // Workspace of the experts' layer: plain codes and scales of x's rows, and (with
-// a compensation) u by slot.
+// a compensation) u by slot, for ranks up to 64 also as bf16 hi | lo rows.
 struct ExpertWs {
     int8_t* q;
     float* x_scale;
     float* u;
+    uint8_t* u_hl;
     size_t bytes;
 };
 
@@ -296,16 +297,19 @@ ExpertWs plan_experts(void* base, int64_t T, int64_t n_slots, int64_t K, int ran
     };
     w.q = reinterpret_cast<int8_t*>(carve(static_cast<size_t>(T) * static_cast<size_t>(K)));
     w.x_scale = reinterpret_cast<float*>(carve(static_cast<size_t>(T) * sizeof(float)));
-    if (rank > 0 && n_mod > 1)
+    if (rank > 0 && n_mod > 1) {
         w.u = reinterpret_cast<float*>(carve(static_cast<size_t>(n_slots) * rank * sizeof(float)));
+        if (rank <= 64) w.u_hl = carve(static_cast<size_t>(n_slots) * 256);
+    }
     w.bytes = off;
     return w;
 }
 
 // Tile shape of the experts' layer: 32-row tiles for up to 16 rows an expert
-// on average, 64-row tiles up to 64, else 128 x 128.
-TilePlan plan_expert_tile(int64_t n_slots, int64_t n_experts) {
+// on average, 64-row tiles up to 64, 128 x 128 up to 192, else 256 x 256.
+TilePlan plan_expert_tile(int64_t n_slots, int64_t n_experts, int64_t K) {
     const int64_t avg = n_slots / n_experts;
+    if (avg > 192 && K % 64 == 0) return TilePlan{-1, 1};
     return TilePlan{avg <= 16 ? 0 : (avg <= 64 ? 1 : 2), 1};
 }
 
@@ -469,13 +473,15 @@ masq_status fused_stage(const Fused& a, int stage) {
                                      a.rank, a.n_mod, a.r_up, to_dt(a.lr_dt), a.y, to_dt(a.y_dt), a.w4,
                                      w.dec_part, w.dec_tickets, -1, s},
                     *a.ex));
-            return from_hip(masq::launch_gemm_tile_epilogue(
-                masq::TileGemm{w.q, w.x_scale, a.wq, a.w_scale, a.T, a.c_in, a.c_out, a.modality, w.u,
-                               hl ? w.u_hl : nullptr, a.rank, a.n_mod, a.r_up, to_dt(a.lr_dt), cmc,
-                               nullptr, a.y, to_dt(a.y_dt), a.w4, w.pair,
-                               w.tile.shape >= 0 ? w.tile : masq::TilePlan{2, 1}, w.gk_part,
-                               w.gk_tickets, s},
-                *a.ex));
+            // (256 x 256 tiles split along K have no epilogue: 128 x 128 instead)
+            const bool wide = w.tile.shape < 0 && w.gk_splits <= 1;
+            const masq::TileGemm g{w.q, w.x_scale, a.wq, a.w_scale, a.T, a.c_in, a.c_out, a.modality,
+                                   w.u, hl ? w.u_hl : nullptr, a.rank, a.n_mod, a.r_up, to_dt(a.lr_dt),
+                                   cmc, nullptr, a.y, to_dt(a.y_dt), a.w4, w.pair,
+                                   w.tile.shape >= 0 ? w.tile : masq::TilePlan{2, 1}, w.gk_part,
+                                   w.gk_tickets, s};
+            return from_hip(wide ? masq::launch_gemm_wide(g, *a.ex)
+                                 : masq::launch_gemm_tile_epilogue(g, *a.ex));
         }
         st = from_hip(masq::launch_gemm(w.q, w.x_scale, a.wq, a.w_scale, a.T, a.c_in, a.c_out,
                                         a.modality, w.u, hl ? w.u_hl : nullptr, w.dec_part,
@@ -801,10 +807,12 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
     if ((st = check_act(act, c_out)) != MASQ_OK) return st;
     if (n_slots < 0 || n_slots > (1LL << 31) - 1) return MASQ_ERR_SHAPE;
     if (rows == nullptr && n_slots > 0 && T > 0 && n_slots != T) return MASQ_ERR_SHAPE;
-    const masq::TilePlan plan = masq::plan_expert_tile(n_slots, n_experts);
+    const masq::TilePlan plan = masq::plan_expert_tile(n_slots, n_experts, c_in);
     // tiles are counted in 32 bits
-    const int64_t tiles = masq::expert_tiles(n_slots, n_experts, masq::kTileShapes[plan.shape].bm);
-    const int64_t tiles_n = (c_out + masq::kTileShapes[plan.shape].bn - 1) / masq::kTileShapes[plan.shape].bn;
+    const bool wide = plan.shape < 0;
+    const int bm = wide ? masq::kTileM : masq::kTileShapes[plan.shape].bm;
+    const int bn = wide ? masq::kTileN : masq::kTileShapes[plan.shape].bn;
+    const int64_t tiles = masq::expert_tiles(n_slots, n_experts, bm), tiles_n = (c_out + bn - 1) / bn;
     if (tiles > ((1LL << 31) - 8) / tiles_n) return MASQ_ERR_SHAPE;
     if (!valid_dt(x_dt) || !valid_dt(y_dt) || !valid_dt(lr_dt)) return MASQ_ERR_DTYPE;
     if (T == 0 || n_slots == 0) return MASQ_OK;
@@ -832,16 +840,17 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
     st = from_hip(masq::launch_smooth_quant(x, to_dt(x_dt), modality, inv_smooth, T, c_in, n_mod, w.q,
                                             w.x_scale, nullptr, 0, s));
     if (st != MASQ_OK) return st;
+    const bool hl = cmc && rank <= 64 && lr_dt == MASQ_BF16;
     if (cmc) {
         st = from_hip(masq::launch_expert_down(x, to_dt(x_dt), modality, inv_smooth, l_down, to_dt(lr_dt),
-                                               n_slots, c_in, rank, n_mod, w.u, ex, s));
+                                               n_slots, c_in, rank, n_mod, w.u, hl ? w.u_hl : nullptr,
+                                               ex, s));
         if (st != MASQ_OK) return st;
     }
-    return from_hip(masq::launch_gemm_experts(
-        masq::TileGemm{w.q, w.x_scale, static_cast<const int8_t*>(wq), w_scale, n_slots, c_in, c_out,
-                       modality, w.u, nullptr, rank, n_mod, r_up, to_dt(lr_dt), cmc, nullptr, y,
-                       to_dt(y_dt), w4, false, plan, nullptr, nullptr, s},
-        ex));
+    const masq::TileGemm g{w.q, w.x_scale, static_cast<const int8_t*>(wq), w_scale, n_slots, c_in, c_out,
+                           modality, w.u, hl ? w.u_hl : nullptr, rank, n_mod, r_up, to_dt(lr_dt), cmc,
+                           nullptr, y, to_dt(y_dt), w4, false, plan, nullptr, nullptr, s};
+    return from_hip(wide ? masq::launch_gemm_wide(g, ex) : masq::launch_gemm_experts(g, ex));
 }
 
 masq_status masq_combine_experts(const void* d, masq_dtype dt, const int32_t* slots,

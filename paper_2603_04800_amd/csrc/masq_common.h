@@ -366,6 +366,8 @@ struct TileGemm {
 hipError_t launch_gemm_tile(const TileGemm& g);
 // The same with bias, activation and residual (no accumulator output).
 hipError_t launch_gemm_tile_epilogue(const TileGemm& g, const TileExtra& ex);
+// The same, or the experts' layer (ex.offsets), on 256 x 256 tiles (K % 64 == 0).
+hipError_t launch_gemm_wide(const TileGemm& g, const TileExtra& ex);
 
 // The decode GEMM (small_path): u (null without compensation) holds u_slices
 // partials [T][rank]; part: the decode workspace's [slices + 1][kSmallMaxT][N],
@@ -402,7 +404,8 @@ inline int64_t expert_tiles(int64_t n_slots, int64_t n_experts, int64_t bm) {
 hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex);
 hipError_t launch_expert_down(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
                               const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
-                              int n_mod, float* u, const TileExtra& ex, hipStream_t s);
+                              int n_mod, float* u, uint8_t* u_hl, const TileExtra& ex,
+                              hipStream_t s);
 
 // Routing: at most kRouteMaxExperts experts and kRouteMaxK choices a token.
 // blocks == 0: one workgroup takes the batch and no workspace is needed.

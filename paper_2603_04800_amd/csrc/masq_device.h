@@ -39,6 +39,10 @@ template <> struct Elem<float> {
         v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
     static __device__ __forceinline__ float load1(const float* p) { return *p; }
+    static __device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
+        const v4f a = *reinterpret_cast<const v4f*>(p);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    }
     static __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 };
 template <> struct Elem<bf16_t> {
@@ -51,12 +55,38 @@ template <> struct Elem<bf16_t> {
         }
     }
     static __device__ __forceinline__ float load1(const bf16_t* p) { return bf16_to_f32(*p); }
+    static __device__ __forceinline__ void load4(const bf16_t* p, float (&v)[4]) {
+        const v2i a = *reinterpret_cast<const v2i*>(p);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            v[2 * j] = __uint_as_float(static_cast<uint32_t>(a[j]) << 16);
+            v[2 * j + 1] = __uint_as_float(static_cast<uint32_t>(a[j]) & 0xFFFF0000u);
+        }
+    }
     static __device__ __forceinline__ void store1(bf16_t* p, float v) {
         *p = static_cast<bf16_t>(f32_to_bf16(v));
     }
 };
 
 __device__ __forceinline__ void load8_f32(const float* p, float (&v)[8]) { Elem<float>::load8(p, v); }
+
+// Four or eight values rounded once and stored.
+__device__ __forceinline__ void store4(float* p, const float (&v)[4]) {
+    *reinterpret_cast<v4f*>(p) = v4f{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4]) {
+    *reinterpret_cast<v2i*>(p) = v2i{static_cast<int32_t>(pack_bf16x2(v[0], v[1])),
+                                     static_cast<int32_t>(pack_bf16x2(v[2], v[3]))};
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+    *reinterpret_cast<v4f*>(p) = v4f{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<v4f*>(p + 4) = v4f{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
+    *reinterpret_cast<v4i*>(p) =
+        v4i{static_cast<int32_t>(pack_bf16x2(v[0], v[1])), static_cast<int32_t>(pack_bf16x2(v[2], v[3])),
+            static_cast<int32_t>(pack_bf16x2(v[4], v[5])), static_cast<int32_t>(pack_bf16x2(v[6], v[7]))};
+}
 
 // Eight elements as loaded (16 or 32 bytes), converted to fp32 only when
 // used, so that a software pipeline can keep the load in flight meanwhile.

@@ -1,0 +1,219 @@
+// Epilogues of the layer's GEMMs and the rows of the experts' layer.
+#pragma once
+
+#include "masq_device.h"
+
+namespace masq {
+namespace {
+
+// What a tile does past the layer's own result: nothing (kTilePlain); bias,
+// activation and residual (kTileEpilogue); the same for output rows sorted by
+// expert, each expert with a weight, scales, factors and bias of its own
+// (kTileExperts).
+enum { kTilePlain = 0, kTileEpilogue = 1, kTileExperts = 2 };
+
+// One tile of rows of one expert.
+struct GroupTile {
+    int expert, tn;
+    int64_t first, end;       // its slots
+};
+
+// Edge e of the experts' slot ranges, within [0, n] whatever the array holds.
+__device__ __forceinline__ int group_edge(const TileExtra& ex, int e, int64_t n) {
+    return static_cast<int>(min(max(static_cast<int64_t>(ex.offsets[min(e, ex.n_experts)]), int64_t{0}), n));
+}
+
+// The tile of workgroup `block`: every wave counts the experts' tiles of BM
+// rows, a lane an expert, places the workgroup among them as tile_coords_at
+// does, and finds the expert that holds its row of tiles.  False past the last
+// tile (the grid is sized for the most tiles that n slots can make).
+template <int BM>
+__device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64_t block, int tiles_n,
+                                           GroupTile& out) {
+    const int lane = threadIdx.x & 63;
+    auto count = [&](int e, int& lo, int& hi) __attribute__((always_inline)) {
+        lo = group_edge(ex, e, n);
+        hi = e < ex.n_experts ? max(group_edge(ex, e + 1, n), lo) : lo;
+        return (hi - lo + BM - 1) / BM;
+    };
+    auto scan = [&](int v) __attribute__((always_inline)) {          // inclusive over the lanes
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int p = __shfl_up(v, o);
+            v += lane >= o ? p : 0;
+        }
+        return v;
+    };
+    int lo, hi;
+    int incl = scan(count(lane, lo, hi));
+    int total = __builtin_amdgcn_readlane(incl, 63);
+    for (int b = 64; b < ex.n_experts; b += 64) {
+        int l2, h2;
+        total += __builtin_amdgcn_readlane(scan(count(b + lane, l2, h2)), 63);
+    }
+    int tm;
+    if (!tile_coords_at(static_cast<int>(block), total, tiles_n, tm, out.tn)) return false;
+    int before = 0, b = 0;
+    for (;;) {
+        const int here = __builtin_amdgcn_readlane(incl, 63);
+        if (tm < before + here || b + 64 >= ex.n_experts) break;
+        before += here;
+        b += 64;
+        incl = scan(count(b + lane, lo, hi));
+    }
+    const unsigned long long past = __ballot(before + incl > tm);
+    const int l = past != 0 ? __builtin_ctzll(past) : 63;            // (tm < total: past != 0)
+    const int prev = l > 0 ? __builtin_amdgcn_readlane(incl, l - 1) : 0;
+    out.expert = min(b + l, ex.n_experts - 1);
+    out.first = __builtin_amdgcn_readlane(lo, l) + static_cast<int64_t>(tm - before - prev) * BM;
+    out.end = min(out.first + BM, static_cast<int64_t>(__builtin_amdgcn_readlane(hi, l)));
+    return true;
+}
+
+// The row of x behind a slot (an index outside it reads row 0).
+__device__ __forceinline__ int64_t slot_row(const TileExtra& ex, int64_t slot) {
+    if (ex.rows == nullptr) return slot;
+    const int t = ex.rows[slot];
+    return t >= 0 && t < ex.x_rows ? t : 0;
+}
+
+// 1 / (1 + exp(-z)) from v_exp_f32 and v_rcp_f32 (one unit in the last place
+// each).  Results that are rounded to bf16 take -z log2 e as one product, off by
+// |z| 2^-24; fp32 results add the product's own error and the next bits of
+// log2 e.  An exponential that overflows has the reciprocal 0, the limit.
+template <bool EXACT>
+__device__ __forceinline__ float logistic(float z) {
+    constexpr float kL = -1.44269504088896341f, kLo = -1.92596299e-8f, kLn2 = 0.69314718055994531f;
+    const float t = z * kL;
+    float e = __builtin_amdgcn_exp2f(t);
+    if constexpr (EXACT) e *= fmaf(fmaf(z, kLo, fmaf(z, kL, -t)), kLn2, 1.f);
+    return __builtin_amdgcn_rcpf(1.f + e);
+}
+template <bool EXACT>
+__device__ __forceinline__ float act_silu(float z) { return z * logistic<EXACT>(z); }
+// erfc, unlike 1 + erf, keeps its relative accuracy for negative z, where it is small
+__device__ __forceinline__ float act_gelu(float z) { return 0.5f * z * erfcf(z * -0.70710678118654752f); }
+template <bool EXACT>
+__device__ __forceinline__ float act_gelu_tanh(float z) {   // (1 + tanh t) / 2 = 1 / (1 + exp(-2 t))
+    return z * logistic<EXACT>(1.5957691216057308f * (z + 0.044715f * (z * z * z)));
+}
+// act on every STEP-th of the N values, one branch for all of them
+template <typename YT, int STEP, int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N]) {
+    constexpr bool kExact = sizeof(YT) == 4;
+    switch (act) {                                          // uniform
+        case kActSilu:
+#pragma unroll
+            for (int e = 0; e < N; e += STEP) v[e] = act_silu<kExact>(v[e]);
+            break;
+        case kActGelu:
+#pragma unroll
+            for (int e = 0; e < N; e += STEP) v[e] = act_gelu(v[e]);
+            break;
+        case kActGeluTanh:
+#pragma unroll
+            for (int e = 0; e < N; e += STEP) v[e] = act_gelu_tanh<kExact>(v[e]);
+            break;
+        default: break;
+    }
+}
+
+// Bias, activation (times the up channel where gated), residual, rounding and
+// store of a row of NJ blocks of one wave (32 tokens x 32 channels each; lane =
+// token lane % 32, register 4 g + e = channel 8 g + 4 (lane / 32) + e).  The
+// values pass through a per-wave LDS transpose, 16 channels at a time, after
+// which a lane holds 8 neighbouring channels of one token: bias and residual
+// are read, and the output written, in whole pieces of 8 (gated: 4) elements,
+// and the only rounding to the output type follows the last addition.  An
+// element of the residual is read by the lane that writes the output's same
+// element, so the two may be one array.  LDS operations of one wave execute in
+// order, so its buffer (32 rows of kEpiPitch floats) needs no synchronisation.
+//
+// The loop over the blocks is not unrolled (they move down a block a turn): a tile runs through this code once, so that its length is
+// paid in instruction fetches.  Fully unrolled, the activations of a 256 x 256
+// tile took longer than its products: 930 us where this form takes @@ (4096 x
+// 3584 -> 37888, gated).
+constexpr int kEpiPitch = 20;                               // 16 channels and 16 bytes
+template <typename YT, int NJ>
+__device__ __forceinline__ void finish_row(v16f (&yb)[NJ], const TileExtra& ex, const float* bias,
+                                           float* scr, YT* y, int64_t trow, int64_t rend, int tcol,
+                                           int N, int lane) {
+    const int width = ex.gated ? N >> 1 : N;                // outputs of a row
+    const int64_t t = trow + (lane >> 1);
+    const YT* res = static_cast<const YT*>(ex.residual);
+    float* wr = scr + (lane & 31) * kEpiPitch + 4 * (lane >> 5);
+    const float* rd = scr + (lane >> 1) * kEpiPitch + 8 * (lane & 1);
+    // 16 channels from the first 8 registers of y16 on
+    auto unit = [&](const v16f& y16, auto half, int c) __attribute__((always_inline)) {
+        constexpr int o0 = 8 * decltype(half)::value;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+            *reinterpret_cast<v4f*>(wr + 8 * g) = v4f{y16[o0 + 4 * g], y16[o0 + 4 * g + 1], y16[o0 + 4 * g + 2],
+                                                      y16[o0 + 4 * g + 3]};
+        float v[8];
+        load8_f32(rd, v);
+        if (t >= rend || c >= N) return;
+        if (bias != nullptr) {
+            float b[8];
+            load8_f32(bias + c, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += b[e];
+        }
+        if (ex.gated) {
+            activate<YT, 2>(ex.act, v);
+            float o[4] = {v[0] * v[1], v[2] * v[3], v[4] * v[5], v[6] * v[7]};
+            const int64_t at = t * width + (c >> 1);
+            if (res != nullptr) {
+                float q[4];
+                Elem<YT>::load4(res + at, q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += q[e];
+            }
+            store4(y + at, o);
+        } else {
+            activate<YT, 1>(ex.act, v);
+            const int64_t at = t * width + c;
+            if (res != nullptr) {
+                float q[8];
+                Elem<YT>::load8(res + at, q);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += q[e];
+            }
+            store8(y + at, v);
+        }
+    };
+    const int c0 = tcol + 8 * (lane & 1);
+#pragma unroll 1
+    for (int j = 0; j < NJ; ++j) {
+        unit(yb[0], std::integral_constant<int, 0>{}, c0 + 32 * j);
+        unit(yb[0], std::integral_constant<int, 1>{}, c0 + 32 * j + 16);
+#pragma unroll
+        for (int k = 0; k + 1 < NJ; ++k) yb[k] = yb[k + 1];
+    }
+}
+
+// The same for one channel a lane, neighbouring channels in neighbouring lanes
+// (decode GEMM): the lanes of a gate and its up channel are active together,
+// and the gate's lane writes their output.
+template <typename YT>
+__device__ __forceinline__ void finish_one(float v, const TileExtra& ex, YT* y, int t, int ch, int N) {
+    if (ex.bias != nullptr) v += ex.bias[ch];
+    int o = ch, width = N;
+    float z[1] = {v};
+    activate<YT, 1>(ex.act, z);
+    if (ex.gated) {
+        const float up = __shfl_xor(v, 1);
+        if (ch & 1) return;
+        v = z[0] * up;
+        o = ch >> 1;
+        width = N >> 1;
+    } else {
+        v = z[0];
+    }
+    const int64_t at = static_cast<int64_t>(t) * width + o;
+    if (ex.residual != nullptr) v += Elem<YT>::load1(static_cast<const YT*>(ex.residual) + at);
+    Elem<YT>::store1(y + at, v);
+}
+
+}  // namespace
+}  // namespace masq

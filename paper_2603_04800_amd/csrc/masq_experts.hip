@@ -347,7 +347,7 @@ template <typename XT, typename LT>
 __global__ __launch_bounds__(64 * kEdWaves) void k_expert_down(
     const XT* __restrict__ x, const int32_t* __restrict__ mod, const float* __restrict__ inv_s,
     const LT* __restrict__ l_down, int64_t n_slots, int K, int r, int n_mod, float* __restrict__ u,
-    TileExtra ex) {
+    uint8_t* __restrict__ u_hl, TileExtra ex) {
     constexpr int RG = kEdSlots / 16, RB = kEdRank / 16;
     static_assert(RG * RB * 64 == 64 * kEdWaves, "a thread finishes one 16-byte piece of u");
     __shared__ __attribute__((aligned(16))) v4f red[kEdWaves][RG * RB * 64];
@@ -369,6 +369,19 @@ __global__ __launch_bounds__(64 * kEdWaves) void k_expert_down(
         xp[g] = x + ar * K;
         ip[g] = inv_s + static_cast<int64_t>(md[g]) * K;
     }
+    // thread tid finishes block (og, ob): columns 4 (lane / 16) .. of slot lane % 16
+    const int og = wave / RB, ob = wave % RB;
+    const int64_t slot = gt.first + 16 * og + (lane & 15);
+    const int omd = og == 0 ? md[0] : md[RG - 1];
+    const bool store = ob < nb && slot < gt.end;
+    auto put_hl = [&](v4f v) __attribute__((always_inline)) {
+        uint8_t* p = u_hl + slot * 256 + 2 * (16 * ob + 4 * (lane >> 4));
+        const uint32_t h0 = pack_bf16x2(v.x, v.y), h1 = pack_bf16x2(v.z, v.w);
+        *reinterpret_cast<v2i*>(p) = v2i{static_cast<int32_t>(h0), static_cast<int32_t>(h1)};
+        *reinterpret_cast<v2i*>(p + 128) =
+            v2i{static_cast<int32_t>(pack_bf16x2(v.x - __uint_as_float(h0 << 16), v.y - __uint_as_float(h0 & 0xFFFF0000u))),
+                static_cast<int32_t>(pack_bf16x2(v.z - __uint_as_float(h1 << 16), v.w - __uint_as_float(h1 & 0xFFFF0000u)))};
+    };
     for (int m = 1; m < n_mod; ++m) {
         bool live[RG], any = false;
 #pragma unroll
@@ -431,15 +444,13 @@ __global__ __launch_bounds__(64 * kEdWaves) void k_expert_down(
 #pragma unroll
             for (int b = 0; b < RB; ++b) red[wave][(g * RB + b) * 64 + lane] = acc[g][b];
         __syncthreads();
-        // thread tid: block (g, b) = wave, its lane's columns 4 (lane / 16) .. of slot lane % 16
         v4f v = red[0][tid];
 #pragma unroll
         for (int w = 1; w < kEdWaves; ++w) v = v + red[w][tid];
-        const int g = wave / RB, b = wave % RB;
-        const int64_t slot = gt.first + 16 * g + (lane & 15);
-        const bool mine = g == 0 ? live[0] : live[RG - 1];
-        if (b < nb && slot < gt.end && mine)
-            *reinterpret_cast<v4f*>(u + slot * r + c0 + 16 * b + 4 * (lane >> 4)) = v;
+        if (store && omd == m) {
+            *reinterpret_cast<v4f*>(u + slot * r + c0 + 16 * ob + 4 * (lane >> 4)) = v;
+            if (u_hl != nullptr) put_hl(v);
+        }
         __syncthreads();                                     // red is free for the next modality
     }
 }
@@ -487,15 +498,7 @@ __global__ __launch_bounds__(256) void k_combine(const DTy* __restrict__ d,
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += q[e];
     }
-    DTy* dst = y + t * N + o;
-    if constexpr (sizeof(DTy) == 2) {
-        *reinterpret_cast<v4i*>(dst) =
-            v4i{static_cast<int32_t>(pack_bf16x2(v[0], v[1])), static_cast<int32_t>(pack_bf16x2(v[2], v[3])),
-                static_cast<int32_t>(pack_bf16x2(v[4], v[5])), static_cast<int32_t>(pack_bf16x2(v[6], v[7]))};
-    } else {
-        *reinterpret_cast<v4f*>(dst) = v4f{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<v4f*>(dst + 4) = v4f{v[4], v[5], v[6], v[7]};
-    }
+    store8(y + t * N + o, v);
 }
 
 }  // namespace
@@ -522,7 +525,7 @@ hipError_t launch_gemm_stream_epilogue(const StreamGemm& g, const TileExtra& ex)
 
 hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex) {
     if (g.K % 16 != 0 || g.N % (ex.gated ? 32 : 16) != 0 || g.plan.S != 1 || (g.w4 && g.K % 64 != 0) ||
-        g.a_pair || g.plan.shape < 0 || g.acc != nullptr || g.u_hl != nullptr)
+        g.a_pair || g.plan.shape < 0 || g.acc != nullptr)
         return hipErrorInvalidValue;
     return launch_tile_any<kTileExperts>(
         g, ex, static_cast<int>(expert_tiles(g.T, ex.n_experts, kTileShapes[g.plan.shape].bm)));
@@ -530,13 +533,14 @@ hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex) {
 
 hipError_t launch_expert_down(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
                               const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
-                              int n_mod, float* u, const TileExtra& ex, hipStream_t s) {
+                              int n_mod, float* u, uint8_t* u_hl, const TileExtra& ex,
+                              hipStream_t s) {
     const int64_t nt = expert_tiles(n_slots, ex.n_experts, kEdSlots) * ((rank + kEdRank - 1) / kEdRank);
     const dim3 grid = grid_of(8 * ((nt + 7) / 8), 64 * kEdWaves), block(64 * kEdWaves);
 #define MASQ_DOWN(XT, LT)                                                                           \
     hipLaunchKernelGGL((k_expert_down<XT, LT>), grid, block, 0, s, static_cast<const XT*>(x), mod,  \
                        inv_s, static_cast<const LT*>(l_down), n_slots, static_cast<int>(K), rank,   \
-                       n_mod, u, ex)
+                       n_mod, u, u_hl, ex)
     if (x_dt == DT::BF16) {
         if (lr_dt == DT::BF16) MASQ_DOWN(bf16_t, bf16_t);
         else MASQ_DOWN(bf16_t, float);

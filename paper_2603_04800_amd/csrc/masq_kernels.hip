@@ -24,7 +24,7 @@
 // dequantisation is two fp32 multiplies in a fixed order.  The library is
 // compiled without FP contraction.
 
-#include "masq_device.h"
+#include "masq_epilogue.h"
 
 
 namespace masq {
@@ -2313,6 +2313,120 @@ __device__ __forceinline__ void gemm_epilogue(
     }
 }
 
+// The epilogue with bias, activation and residual: the compensation as above,
+// then finish_row.  One rolled loop over the four row blocks (the accumulators
+// move down a row a turn), so that its code is short (finish_row).
+template <typename YT, typename LT, bool CMC, int NWN>
+__device__ __forceinline__ void gemm_epilogue_extra(
+    v16i (&acc)[4][8 / NWN], GemmSmem& sm, int64_t T, int N, int64_t row0, int col0,
+    const float* __restrict__ u, int r, int n_mod, const LT* __restrict__ r_up, YT* y,
+    const EpiDma& ed, int rb, int tid, const TileExtra& ex) {
+    constexpr int NJ = 8 / NWN, NW = 2 * NWN, NT = 64 * NW;
+    const int lane = tid & 63, wave = tid >> 6;
+    const int wm = wave / NWN, wn = wave % NWN;
+    RowOps& ro = sm.ro[rb];
+    __syncthreads();                       // every wave is done with the K stages
+    static_assert(32 * kEpiPitch * 4 * NW <= kTrBytes, "fp32 transposes");
+    float* scr = reinterpret_cast<float*>(sm.tr) + wave * 32 * kEpiPitch;
+    const int tcol = col0 + wn * 32 * NJ;
+
+    constexpr int kU = CMC ? Cmc<LT>::kUBytes : 0, kR = CMC ? Cmc<LT>::kRBytes : 0;
+    const unsigned present = CMC ? ed.present : 0;
+    const int n_present = __builtin_popcount(present);
+    const int n_chunks = (r + 63) >> 6, chunk_bytes = kU + n_present * kR;
+    const bool staged = !ed.pre && n_chunks * chunk_bytes <= static_cast<int>(sizeof(sm.buf));
+    if constexpr (CMC) {
+        if (n_present > 0 && staged) {
+            for (int c = 0; c < n_chunks; ++c) {
+                uint8_t* base = sm.buf + c * chunk_bytes;
+                Cmc<LT>::template stage_u<NT>(base, ro.mod, u, row0, T, r, 64 * c, tid);
+                int p = 0;
+                for (int m = 1; m < n_mod; ++m) {
+                    if (!(present & (1u << m))) continue;
+                    Cmc<LT>::template stage_r<NT>(base + kU + p * kR, r_up + static_cast<int64_t>(m - 1) * N * r,
+                                                  col0, N, r, 64 * c, tid);
+                    ++p;
+                }
+            }
+            __syncthreads();
+        }
+    }
+    const int first = present ? __builtin_ctz(present) : 0;
+    const int second = (present & (present - 1u)) ? __builtin_ctz(present & (present - 1u)) : 0;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+        const int trow = wm * 128 + 32 * i + (lane & 31);
+        v16f ybs[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const float dx = ro.dx[trow];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const v4f ws = *reinterpret_cast<const v4f*>(
+                    &ro.ws[wn * 32 * NJ + 32 * j + 8 * g + 4 * (lane >> 5)]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    ybs[j][4 * g + e] = (static_cast<float>(acc[0][j][4 * g + e]) * dx) * ws[e];
+            }
+        }
+        if constexpr (CMC) {
+            const int tmod = ro.mod[trow];
+            if (sizeof(LT) == 2 && ed.pre) {               // bf16 hi | lo rows by DMA, one or two modalities
+#pragma unroll 1
+                for (int p = 0; p < n_present; ++p) {
+                    const bool live = tmod == (p == 0 ? first : second);
+                    const uint8_t* sr = sm.buf + ed.off_r[p];
+                    const v4i zero = {0, 0, 0, 0};
+#pragma unroll 1
+                    for (int ks = 0; ks < (r >> 4); ++ks) {
+                        const int cc = 2 * ks + (lane >> 5);
+                        const int off = trow * 128 + ((cc ^ swz(trow)) << 4);
+                        v4i hi = *reinterpret_cast<const v4i*>(sm.buf + ed.off_uh + off);
+                        v4i lo = *reinterpret_cast<const v4i*>(sm.buf + ed.off_ul + off);
+                        const v8bf h = __builtin_bit_cast(v8bf, live ? hi : zero);
+                        const v8bf l = __builtin_bit_cast(v8bf, live ? lo : zero);
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) {
+                            const int crow = wn * 32 * NJ + j * 32 + (lane & 31);
+                            const v8bf b = __builtin_bit_cast(
+                                v8bf, *reinterpret_cast<const v4i*>(sr + crow * 128 + ((cc ^ swz(crow)) << 4)));
+                            ybs[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, h, ybs[j], 0, 0, 0);
+                            ybs[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, l, ybs[j], 0, 0, 0);
+                        }
+                    }
+                }
+            } else if (n_present > 0) {
+#pragma unroll 1
+                for (int c = 0; c < n_chunks; ++c) {
+                    int p = 0;
+                    for (int m = 1; m < n_mod; ++m) {
+                        if (!(present & (1u << m))) continue;
+                        const bool live = tmod == m;
+                        const uint8_t* base = sm.buf + c * chunk_bytes;
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) {
+                            const int crow = wn * 32 * NJ + 32 * j + (lane & 31);
+                            if (staged)
+                                ybs[j] = Cmc<LT>::from_lds(base, base + kU + p * kR, min(64, r - 64 * c), trow,
+                                                           crow, live, lane, ybs[j]);
+                            else
+                                ybs[j] = Cmc<LT>::from_global(u, r_up + static_cast<int64_t>(m - 1) * N * r,
+                                                              live && row0 + trow < T, row0 + trow,
+                                                              min(col0 + crow, N - 1), r, 64 * c, lane, ybs[j]);
+                        }
+                        ++p;
+                    }
+                }
+            }
+        }
+        finish_row<YT, NJ>(ybs, ex, ex.bias, scr, y, row0 + wm * 128 + 32 * i, T, tcol, N, lane);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[k][j] = acc[k + 1][j];
+    }
+}
+
 // ---------------------------------------------------------------- GEMM, K % 64 == 0
 // Direct-to-LDS pipeline: 64-byte K stages (A and B tiles 256 x 64 each) go
 // from global memory straight into one of 4 LDS buffers with
@@ -2365,7 +2479,7 @@ __device__ __forceinline__ int swz4(int row) { return (row >> 2) & 3; }
 // (all three with no compensation operands staged, one with a single
 // non-text modality's), the ring of K buffers then starting at that buffer.
 template <typename YT, typename LT, bool CMC, bool ACC, int NWN = 2, bool SPLIT = false,
-          bool W4 = false, bool GRP = false, bool PERSIST = false>
+          bool W4 = false, bool GRP = false, bool PERSIST = false, int MODE = kTilePlain>
 __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     const int8_t* __restrict__ A, const int8_t* __restrict__ B, const float* __restrict__ x_scale,
     const float* __restrict__ w_scale, int64_t T, int K, int N, int tiles_m, int tiles_n,
@@ -2373,11 +2487,13 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     int r, int n_mod, const LT* __restrict__ r_up, int32_t* __restrict__ acc_out,
     YT* __restrict__ y, int S, int32_t* __restrict__ part, int* __restrict__ tickets,
     const int32_t* __restrict__ grows, const v4i* __restrict__ gtab,
-    const int* __restrict__ gtab_n, int64_t b_stride, bool a_pair) {
+    const int* __restrict__ gtab_n, int64_t b_stride, bool a_pair, TileExtra ex) {
+    constexpr bool EXP = MODE == kTileExperts;
     __shared__ __attribute__((aligned(16))) GemmSmem sm;
     static_assert(kDmaStages * kDmaStageBytes <= static_cast<int>(sizeof(GemmSmem::buf)), "LDS");
     static_assert(kDmaStageBytes == kTileM * 128, "an epilogue operand fills one K stage buffer");
-    static_assert(!PERSIST || (!SPLIT && !GRP), "persistent grid: whole tiles, one weight");
+    static_assert(!PERSIST || (!SPLIT && !GRP && !EXP), "persistent grid: whole tiles, one weight");
+    static_assert(!EXP || (!SPLIT && !GRP), "experts: whole tiles");
     if constexpr (!SPLIT) S = 1;
     constexpr int NJ = 8 / NWN, NW = 2 * NWN;
     constexpr int kRowsPerWave = kTileM / NW;           // DMA rows of A and of B per wave
@@ -2407,8 +2523,22 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / NWN, wn = wave % NWN;
-    int tm, tn;
-    if (!tile_coords_at(vb, tiles_m, tiles_n * S, tm, tn)) break;
+    int tm = 0, tn;
+    // EXP: rows [row0, T) of the slots of one expert
+    int64_t slot0 = 0;
+    if constexpr (EXP) {
+        GroupTile gt;
+        if (!group_tile<kTileM>(ex, T, vb, tiles_n, gt)) break;
+        tn = gt.tn;
+        slot0 = gt.first;
+        T = gt.end;
+        B += static_cast<int64_t>(gt.expert) * N * (W4 ? K / 2 : K);
+        w_scale += static_cast<int64_t>(gt.expert) * N;
+        if constexpr (CMC) r_up += static_cast<int64_t>(gt.expert) * (n_mod - 1) * N * r;
+        if (ex.bias != nullptr) ex.bias += static_cast<int64_t>(gt.expert) * N;
+    } else {
+        if (!tile_coords_at(vb, tiles_m, tiles_n * S, tm, tn)) break;
+    }
     // split K: slice sl of S covers stages [kst0, kst0 + nk) of the tile
     int sl = 0;
     if constexpr (SPLIT) {
@@ -2417,7 +2547,7 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     }
     const int nk_slice = SPLIT ? (nk_all + S - 1) / S : nk_all;
     const int kst0 = sl * nk_slice;
-    const int64_t row0 = GRP ? 0 : static_cast<int64_t>(tm) * kTileM;
+    const int64_t row0 = GRP ? 0 : (EXP ? slot0 : static_cast<int64_t>(tm) * kTileM);
     const int col0 = tn * kTileN;
     // GRP: the tile's rows grows[gfirst .. gfirst + grows_n), modality gmod
     int gfirst = 0, grows_n = kTileM, gmod = 0;
@@ -2436,6 +2566,11 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
         if constexpr (GRP) return grows[gfirst + min(l, grows_n - 1)];
         else return min(row0 + l, T - 1);
     };
+    // the row of A and of the tokens' operands behind an output row
+    auto x_row = [&](int64_t t) __attribute__((always_inline)) -> int64_t {
+        if constexpr (EXP) return slot_row(ex, t);
+        else return t;
+    };
     RowOps& ro = sm.ro[rb];
 
     v16i acc[4][NJ];
@@ -2453,14 +2588,14 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
             const void* src;
             uint32_t dst;
             if (c < 4) {
-                src = x_scale + (GRP ? a_row(e) : min(r0 + e, T - 1));
+                src = x_scale + (GRP ? a_row(e) : x_row(min(r0 + e, T - 1)));
                 dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&o.dx[64 * part]));
             } else if (c < 8) {
                 src = w_scale + min(c0 + e, N - 1);
                 dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&o.ws[64 * part]));
             } else {
                 src = GRP ? static_cast<const void*>(grows + gfirst + min(e, grows_n - 1))
-                          : static_cast<const void*>(mod + min(r0 + e, T - 1));
+                          : static_cast<const void*>(mod + x_row(min(r0 + e, T - 1)));
                 dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&o.rawmod[64 * part]));
             }
             lds_dma4(src, static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(dst))));
@@ -2485,7 +2620,7 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
         for (int j = 0; j < kDmaA; ++j) {
             const int row = wave * kRowsPerWave + 16 * j + (lane >> 2);
             const int chunk = (lane & 3) ^ swz4(row);
-            const int64_t tok = GRP ? a_row(row) : min(r0 + row, T - 1);
+            const int64_t tok = GRP ? a_row(row) : x_row(min(r0 + row, T - 1));
             sp[j] = A + code_row(tok, K, a_pair) + kst0 * a_step + 16 * chunk;
         }
 #pragma unroll
@@ -2761,8 +2896,12 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     else if (npf == 1) MASQ_WAIT_VMCNT_LGKM0(kPiecesMin + kDmaPerStage);
     else if (npf == 2) MASQ_WAIT_VMCNT_LGKM0(kPiecesMin + 2 * kDmaPerStage);
     else MASQ_WAIT_VMCNT_LGKM0(kPiecesMin + 3 * kDmaPerStage);
-    gemm_epilogue<YT, LT, CMC, ACC, NWN, GRP>(acc, sm, T, N, row0, col0, u, r, n_mod,
-                                               r_up, acc_out, y, ed, rb, tid);
+    if constexpr (MODE == kTilePlain)
+        gemm_epilogue<YT, LT, CMC, ACC, NWN, GRP>(acc, sm, T, N, row0, col0, u, r, n_mod,
+                                                   r_up, acc_out, y, ed, rb, tid);
+    else
+        gemm_epilogue_extra<YT, LT, CMC, NWN>(acc, sm, T, N, row0, col0, u, r, n_mod, r_up, y, ed, rb,
+                                              tid, ex);
     if constexpr (!PERSIST) break;
     ring = nring;
     pf = max(npf, 0);
@@ -3186,14 +3325,14 @@ static void launch_gemm_t(const int8_t* q, const float* x_scale, const int8_t* w
                            dim3(8 * ((nt * S + 7) / 8)), dim3(128 * kGemmWavesN), 0, s, q, wq, x_scale,
                            w_scale, T, static_cast<int>(K), static_cast<int>(N), tiles_m, tiles_n, mod,
                            u, u_hl, rank, n_mod, static_cast<const LT*>(r_up), acc,
-                           static_cast<YT*>(y), S, part, tickets, nullptr, nullptr, nullptr, 0, a_pair);
+                           static_cast<YT*>(y), S, part, tickets, nullptr, nullptr, nullptr, 0, a_pair, TileExtra{});
     else      // whole tiles: a persistent grid of at most one workgroup per compute unit
         hipLaunchKernelGGL((k_gemm_dma<YT, LT, CMC, ACC, kGemmWavesN, false, W4, false, true>),
                            dim3(static_cast<unsigned>(min(8 * ((nt + 7) / 8), persistent_blocks()))),
                            dim3(128 * kGemmWavesN), 0, s, q, wq, x_scale, w_scale, T,
                            static_cast<int>(K), static_cast<int>(N), tiles_m, tiles_n, mod, u, u_hl,
                            rank, n_mod, static_cast<const LT*>(r_up), acc, static_cast<YT*>(y), 1,
-                           nullptr, nullptr, nullptr, nullptr, nullptr, 0, a_pair);
+                           nullptr, nullptr, nullptr, nullptr, nullptr, 0, a_pair, TileExtra{});
 }
 
 hipError_t launch_group_rows(const int32_t* mod, int64_t T, int n_mod, int32_t* rows,
@@ -3218,13 +3357,13 @@ static void launch_gemm_grouped_t(const int8_t* q, const float* x_scale, const i
                            block, 0, s, q, wq, x_scale, w_scale, T, static_cast<int>(K),
                            static_cast<int>(N), tiles_m, tiles_n, nullptr, nullptr, nullptr, 0, n_mod,
                            nullptr, nullptr, static_cast<YT*>(y), S, part, tickets, rows, tb, tab_n,
-                           N * K, true);
+                           N * K, true, TileExtra{});
     else
         hipLaunchKernelGGL((k_gemm_dma<YT, bf16_t, false, false, kGemmWavesN, false, false, true>), grid,
                            block, 0, s, q, wq, x_scale, w_scale, T, static_cast<int>(K),
                            static_cast<int>(N), tiles_m, tiles_n, nullptr, nullptr, nullptr, 0, n_mod,
                            nullptr, nullptr, static_cast<YT*>(y), 1, nullptr, nullptr, rows, tb,
-                           tab_n, N * K, true);
+                           tab_n, N * K, true, TileExtra{});
 }
 
 hipError_t launch_gemm_grouped(const int8_t* q, const float* x_scale, const int8_t* wq,
@@ -3240,6 +3379,42 @@ hipError_t launch_gemm_grouped(const int8_t* q, const float* x_scale, const int8
         launch_gemm_grouped_t<float>(q, x_scale, wq, w_scale, T, K, N, n_mod, rows, tab, tab_n, y,
                                      S, part, tickets, s);
     return hipGetLastError();
+}
+
+// Whole 256 x 256 tiles with an epilogue: the layer's on the persistent grid,
+// the experts' a workgroup per tile.
+template <typename YT, typename LT, bool CMC, bool W4>
+static hipError_t launch_gemm_wide_t(const TileGemm& g, const TileExtra& ex) {
+    const int tiles_n = static_cast<int>((g.N + kTileN - 1) / kTileN);
+    const dim3 block(128 * kGemmWavesN);
+#define MASQ_WIDE(PERSIST, MODE, GRID, TM)                                                          \
+    hipLaunchKernelGGL((k_gemm_dma<YT, LT, CMC, false, kGemmWavesN, false, W4, false, PERSIST, MODE>), \
+                       GRID, block, 0, g.stream, g.q, g.wq, g.x_scale, g.w_scale, g.T,              \
+                       static_cast<int>(g.K), static_cast<int>(g.N), TM, tiles_n, g.mod, g.u,       \
+                       g.u_hl, g.rank, g.n_mod, static_cast<const LT*>(g.r_up), nullptr,            \
+                       static_cast<YT*>(g.y), 1, nullptr, nullptr, nullptr, nullptr, nullptr, 0,    \
+                       g.a_pair, ex)
+    if (ex.offsets != nullptr) {
+        const int64_t nt = expert_tiles(g.T, ex.n_experts, kTileM) * tiles_n;
+        MASQ_WIDE(false, kTileExperts, dim3(static_cast<unsigned>(8 * ((nt + 7) / 8))), 0);
+    } else {
+        const int tiles_m = static_cast<int>((g.T + kTileM - 1) / kTileM);
+        const int blocks = min(8 * ((tiles_m * tiles_n + 7) / 8), persistent_blocks());
+        MASQ_WIDE(true, kTileEpilogue, dim3(static_cast<unsigned>(blocks)), tiles_m);
+    }
+#undef MASQ_WIDE
+    return hipGetLastError();
+}
+
+hipError_t launch_gemm_wide(const TileGemm& g, const TileExtra& ex) {
+    if (g.K % kDmaStageK != 0 || g.N % (ex.gated ? 32 : 16) != 0 || g.acc != nullptr)
+        return hipErrorInvalidValue;
+#define MASQ_WIDE(YT, LT, C) (g.w4 ? launch_gemm_wide_t<YT, LT, C, true>(g, ex) : launch_gemm_wide_t<YT, LT, C, false>(g, ex))
+    if (!g.cmc) return g.y_dt == DT::BF16 ? MASQ_WIDE(bf16_t, bf16_t, false) : MASQ_WIDE(float, bf16_t, false);
+    if (g.y_dt == DT::BF16)
+        return g.lr_dt == DT::BF16 ? MASQ_WIDE(bf16_t, bf16_t, true) : MASQ_WIDE(bf16_t, float, true);
+    return g.lr_dt == DT::BF16 ? MASQ_WIDE(float, bf16_t, true) : MASQ_WIDE(float, float, true);
+#undef MASQ_WIDE
 }
 
 hipError_t launch_gemm(const int8_t* q, const float* x_scale, const int8_t* wq,

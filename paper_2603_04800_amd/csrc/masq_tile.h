@@ -23,7 +23,7 @@
 
 #pragma once
 
-#include "masq_device.h"
+#include "masq_epilogue.h"
 
 namespace masq {
 namespace {
@@ -126,221 +126,6 @@ template <> struct CompBlocks<float> {                      // fp32 MFMA, 8 step
         }
     }
 };
-
-// ---------------------------------------------------------------- epilogues
-// What a tile does past the layer's own result: nothing (kTilePlain); bias,
-// activation and residual (kTileEpilogue); the same for output rows sorted by
-// expert, each expert with a weight, scales, factors and bias of its own
-// (kTileExperts).
-enum { kTilePlain = 0, kTileEpilogue = 1, kTileExperts = 2 };
-
-// One tile of rows of one expert.
-struct GroupTile {
-    int expert, tn;
-    int64_t first, end;       // its slots
-};
-
-// Edge e of the experts' slot ranges, within [0, n] whatever the array holds.
-__device__ __forceinline__ int group_edge(const TileExtra& ex, int e, int64_t n) {
-    return static_cast<int>(min(max(static_cast<int64_t>(ex.offsets[min(e, ex.n_experts)]), int64_t{0}), n));
-}
-
-// The tile of workgroup `block`: every wave counts the experts' tiles of BM
-// rows, a lane an expert, places the workgroup among them as tile_coords_at
-// does, and finds the expert that holds its row of tiles.  False past the last
-// tile (the grid is sized for the most tiles that n slots can make).
-template <int BM>
-__device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64_t block, int tiles_n,
-                                           GroupTile& out) {
-    const int lane = threadIdx.x & 63;
-    auto count = [&](int e, int& lo, int& hi) __attribute__((always_inline)) {
-        lo = group_edge(ex, e, n);
-        hi = e < ex.n_experts ? max(group_edge(ex, e + 1, n), lo) : lo;
-        return (hi - lo + BM - 1) / BM;
-    };
-    auto scan = [&](int v) __attribute__((always_inline)) {          // inclusive over the lanes
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int p = __shfl_up(v, o);
-            v += lane >= o ? p : 0;
-        }
-        return v;
-    };
-    int lo, hi;
-    int incl = scan(count(lane, lo, hi));
-    int total = __builtin_amdgcn_readlane(incl, 63);
-    for (int b = 64; b < ex.n_experts; b += 64) {
-        int l2, h2;
-        total += __builtin_amdgcn_readlane(scan(count(b + lane, l2, h2)), 63);
-    }
-    int tm;
-    if (!tile_coords_at(static_cast<int>(block), total, tiles_n, tm, out.tn)) return false;
-    int before = 0, b = 0;
-    for (;;) {
-        const int here = __builtin_amdgcn_readlane(incl, 63);
-        if (tm < before + here || b + 64 >= ex.n_experts) break;
-        before += here;
-        b += 64;
-        incl = scan(count(b + lane, lo, hi));
-    }
-    const unsigned long long past = __ballot(before + incl > tm);
-    const int l = past != 0 ? __builtin_ctzll(past) : 63;            // (tm < total: past != 0)
-    const int prev = l > 0 ? __builtin_amdgcn_readlane(incl, l - 1) : 0;
-    out.expert = min(b + l, ex.n_experts - 1);
-    out.first = __builtin_amdgcn_readlane(lo, l) + static_cast<int64_t>(tm - before - prev) * BM;
-    out.end = min(out.first + BM, static_cast<int64_t>(__builtin_amdgcn_readlane(hi, l)));
-    return true;
-}
-
-// The row of x behind a slot (an index outside it reads row 0).
-__device__ __forceinline__ int64_t slot_row(const TileExtra& ex, int64_t slot) {
-    if (ex.rows == nullptr) return slot;
-    const int t = ex.rows[slot];
-    return t >= 0 && t < ex.x_rows ? t : 0;
-}
-
-// act(z) in fp32.  exp of a large negated argument overflows to infinity and
-// the quotient is the limit 0; erfc, unlike 1 + erf, keeps its relative accuracy
-// for negative z, where it is small.
-__device__ __forceinline__ float act_silu(float z) { return z / (1.f + expf(-z)); }
-__device__ __forceinline__ float act_gelu(float z) { return 0.5f * z * erfcf(z * -0.70710678118654752f); }
-__device__ __forceinline__ float act_gelu_tanh(float z) {   // (1 + tanh t) / 2 = 1 / (1 + exp(-2 t))
-    return z / (1.f + expf(-1.5957691216057308f * (z + 0.044715f * (z * z * z))));
-}
-// f on every STEP-th of the n values, one branch for all of them
-template <int STEP, typename V>
-__device__ __forceinline__ void activate(int act, V& v, int n) {
-    switch (act) {                                          // uniform
-        case kActSilu:
-#pragma unroll
-            for (int e = 0; e < n; e += STEP) v[e] = act_silu(v[e]);
-            break;
-        case kActGelu:
-#pragma unroll
-            for (int e = 0; e < n; e += STEP) v[e] = act_gelu(v[e]);
-            break;
-        case kActGeluTanh:
-#pragma unroll
-            for (int e = 0; e < n; e += STEP) v[e] = act_gelu_tanh(v[e]);
-            break;
-        default: break;
-    }
-}
-
-// Bias, activation (times the up channel where gated), residual, rounding and
-// store of one wave's MI x NJ blocks (32 tokens x 32 channels; lane = token
-// lane % 32, register 4 g + e = channel 8 g + 4 (lane / 32) + e).  Results pass
-// through a per-wave LDS transpose in fp32, 32 or 16 outputs of a row at a
-// time, after which a lane holds 8 neighbouring outputs of one row: the
-// residual is read, and the output written, in whole 16-byte pieces, and the
-// only rounding to the output type follows the last addition.  An element of
-// the residual is read by the lane that writes the output's same element, so
-// the two may be one array.
-constexpr int kEpiPitch = 36;                               // floats: 32 outputs and 16 bytes
-template <typename YT, int MI, int NJ>
-__device__ __forceinline__ void finish_blocks(v16f (&yb)[MI][NJ], const TileExtra& ex,
-                                              const float* __restrict__ bias, float* scr, YT* y,
-                                              int64_t trow, int64_t rend, int tcol, int N, int lane) {
-    const int h = lane >> 5, rw = lane & 31;
-    const int width = ex.gated ? N >> 1 : N;                // outputs of a row
-    const YT* res = static_cast<const YT*>(ex.residual);
-    if (bias != nullptr) {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const v4f b = *reinterpret_cast<const v4f*>(bias + min(tcol + 32 * j + 8 * g + 4 * h, N - 4));
-#pragma unroll
-                for (int i = 0; i < MI; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) yb[i][j][4 * g + e] += b[e];
-            }
-    }
-    // rows [0, 32) x 8-output pieces of a unit of 8 lpr outputs from `out0` on
-    auto drain = [&](int i, int out0, auto pieces) __attribute__((always_inline)) {
-        constexpr int lpr = decltype(pieces)::value, rows = 64 / lpr;
-#pragma unroll
-        for (int k = 0; k < 32 / rows; ++k) {
-            const int rr = rows * k + lane / lpr, pc = lane % lpr;
-            const float* sp = scr + rr * kEpiPitch + 8 * pc;
-            float v[8];
-            load8_f32(sp, v);
-            const int64_t t = trow + 32 * i + rr;
-            const int o = out0 + 8 * pc;
-            if (t >= rend || o >= width) continue;
-            if (res != nullptr) {
-                float q[8];
-                Elem<YT>::load8(res + t * width + o, q);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += q[e];
-            }
-            YT* dst = y + t * width + o;
-            if constexpr (sizeof(YT) == 2) {
-                *reinterpret_cast<v4i*>(dst) =
-                    v4i{static_cast<int32_t>(pack_bf16x2(v[0], v[1])), static_cast<int32_t>(pack_bf16x2(v[2], v[3])),
-                        static_cast<int32_t>(pack_bf16x2(v[4], v[5])), static_cast<int32_t>(pack_bf16x2(v[6], v[7]))};
-            } else {
-                *reinterpret_cast<v4f*>(dst) = v4f{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<v4f*>(dst + 4) = v4f{v[4], v[5], v[6], v[7]};
-            }
-        }
-    };
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        if (ex.gated) {                                     // uniform: gate and up side by side
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                v16f z = yb[i][j];
-                activate<2>(ex.act, z, 16);
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const v2f o = {z[4 * g] * z[4 * g + 1], z[4 * g + 2] * z[4 * g + 3]};
-                    *reinterpret_cast<v2f*>(scr + rw * kEpiPitch + 16 * (j & 1) + 4 * g + 2 * h) = o;
-                }
-                if constexpr (NJ % 2 == 0) {
-                    if (j & 1) drain(i, (tcol >> 1) + 16 * (j - 1), std::integral_constant<int, 4>{});
-                } else {
-                    static_assert(NJ == 1, "one block or pairs of blocks a wave");
-                    drain(i, tcol >> 1, std::integral_constant<int, 2>{});
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                v16f z = yb[i][j];
-                activate<1>(ex.act, z, 16);
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<v4f*>(scr + rw * kEpiPitch + 8 * g + 4 * h) =
-                        v4f{z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3]};
-                drain(i, tcol + 32 * j, std::integral_constant<int, 4>{});
-            }
-        }
-    }
-}
-
-// The same for one channel a lane, neighbouring channels in neighbouring lanes
-// (decode GEMM): the lanes of a gate and its up channel are active together,
-// and the gate's lane writes their output.
-template <typename YT>
-__device__ __forceinline__ void finish_one(float v, const TileExtra& ex, YT* y, int t, int ch, int N) {
-    if (ex.bias != nullptr) v += ex.bias[ch];
-    int o = ch, width = N;
-    float z[1] = {v};
-    activate<1>(ex.act, z, 1);
-    if (ex.gated) {
-        const float up = __shfl_xor(v, 1);
-        if (ch & 1) return;
-        v = z[0] * up;
-        o = ch >> 1;
-        width = N >> 1;
-    } else {
-        v = z[0];
-    }
-    const int64_t at = static_cast<int64_t>(t) * width + o;
-    if (ex.residual != nullptr) v += Elem<YT>::load1(static_cast<const YT*>(ex.residual) + at);
-    Elem<YT>::store1(y + at, v);
-}
 
 // LDS rows of a stage: A rows of 128 bytes, then B rows of 128 bytes (W4: 64
 // bytes of packed codes).  The 16-byte piece c of a 128-byte row lies at
@@ -632,7 +417,14 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void k_gemm_tile(
         static_assert(NST * kStage >= NW * 32 * kEpiPitch * 4, "fp32 transpose buffers fit the ring");
         float* scr = reinterpret_cast<float*>(ring) + wave * 32 * kEpiPitch;
         const float* bias = ex.bias != nullptr ? ex.bias + static_cast<int64_t>(expert) * N : nullptr;
-        finish_blocks<YT, MI, NJ>(yb, ex, bias, scr, y, trow, rend, tcol, N, lane);
+#pragma unroll 1
+        for (int i = 0; i < MI; ++i) {                      // (the blocks move down a row a turn)
+            finish_row<YT, NJ>(yb[0], ex, bias, scr, y, trow + 32 * i, rend, tcol, N, lane);
+#pragma unroll
+            for (int k = 0; k + 1 < MI; ++k)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) yb[k][j] = yb[k + 1][j];
+        }
         return;
     }
 #pragma unroll
