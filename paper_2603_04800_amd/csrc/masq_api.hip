@@ -305,12 +305,23 @@ ExpertWs plan_experts(void* base, int64_t T, int64_t n_slots, int64_t K, int ran
     return w;
 }
 
-// Tile shape of the experts' layer: 32-row tiles for up to 16 rows an expert
-// on average, 64-row tiles up to 64, 128 x 128 up to 192, else 256 x 256.
-TilePlan plan_expert_tile(int64_t n_slots, int64_t n_experts, int64_t K) {
+// Tile shape of the experts' layer, from the rows an expert has on average and
+// the tiles to be expected (half a tile an expert is padding).  Layers of 2048
+// outputs over 64 and 8 experts, 2048 and 1024 columns, us:
+//   32 x 64 / 64 x 64   the weights' stream bounds both; the narrower tile loads
+//       fewer rows of x beside them: packed weights, 8 rows 34.6 / 37.6, 32 rows
+//       39.1 / 43.1; int8 codes 53.0 / 51.7 and 59.6 / 57.8
+//   64 x 64 / 128 x 128  64 rows 77.0 / 76.1 and 41.5 / 46.4, 128 rows 110.7 / 90.4;
+//       with fewer than a tile of 128 x 128 for each compute unit (8 experts of
+//       128 rows, 192 tiles) 22.9 / 25.4
+//   128 x 128 / 256 x 256  256 rows 148.3 / 153.0 and 81.7 / 101.5, 512 rows 47.7 /
+//       42.4 (8 experts), 543.7 / 370.5 (64 experts of 2816 outputs)
+TilePlan plan_expert_tile(int64_t n_slots, int64_t n_experts, int64_t K, int64_t N, bool w4) {
     const int64_t avg = n_slots / n_experts;
-    if (avg > 192 && K % 64 == 0) return TilePlan{-1, 1};
-    return TilePlan{avg <= 16 ? 0 : (avg <= 64 ? 1 : 2), 1};
+    auto tiles = [&](int64_t bm, int64_t bn) { return (n_slots / bm + (n_experts + 1) / 2) * ((N + bn - 1) / bn); };
+    if (avg <= (w4 ? 32 : 8)) return TilePlan{0, 1};
+    if (avg <= 64 || tiles(128, 128) < 256) return TilePlan{1, 1};
+    return TilePlan{avg >= 384 && K % 64 == 0 && tiles(kTileM, kTileN) >= 128 ? -1 : 2, 1};
 }
 
 }  // namespace masq
@@ -807,7 +818,7 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
     if ((st = check_act(act, c_out)) != MASQ_OK) return st;
     if (n_slots < 0 || n_slots > (1LL << 31) - 1) return MASQ_ERR_SHAPE;
     if (rows == nullptr && n_slots > 0 && T > 0 && n_slots != T) return MASQ_ERR_SHAPE;
-    const masq::TilePlan plan = masq::plan_expert_tile(n_slots, n_experts, c_in);
+    const masq::TilePlan plan = masq::plan_expert_tile(n_slots, n_experts, c_in, c_out, w4);
     // tiles are counted in 32 bits
     const bool wide = plan.shape < 0;
     const int bm = wide ? masq::kTileM : masq::kTileShapes[plan.shape].bm;
@@ -837,16 +848,13 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
     ex.n_experts = n_experts;
     ex.x_rows = T;
     (void)hipGetLastError();
-    st = from_hip(masq::launch_smooth_quant(x, to_dt(x_dt), modality, inv_smooth, T, c_in, n_mod, w.q,
-                                            w.x_scale, nullptr, 0, s));
-    if (st != MASQ_OK) return st;
     const bool hl = cmc && rank <= 64 && lr_dt == MASQ_BF16;
-    if (cmc) {
-        st = from_hip(masq::launch_expert_down(x, to_dt(x_dt), modality, inv_smooth, l_down, to_dt(lr_dt),
-                                               n_slots, c_in, rank, n_mod, w.u, hl ? w.u_hl : nullptr,
-                                               ex, s));
-        if (st != MASQ_OK) return st;
-    }
+    st = from_hip(cmc ? masq::launch_expert_stage1(x, to_dt(x_dt), modality, inv_smooth, l_down,
+                                                   to_dt(lr_dt), T, n_slots, c_in, rank, n_mod, w.u,
+                                                   hl ? w.u_hl : nullptr, w.q, w.x_scale, ex, s)
+                      : masq::launch_smooth_quant(x, to_dt(x_dt), modality, inv_smooth, T, c_in, n_mod,
+                                                  w.q, w.x_scale, nullptr, 0, s));
+    if (st != MASQ_OK) return st;
     const masq::TileGemm g{w.q, w.x_scale, static_cast<const int8_t*>(wq), w_scale, n_slots, c_in, c_out,
                            modality, w.u, hl ? w.u_hl : nullptr, rank, n_mod, r_up, to_dt(lr_dt), cmc,
                            nullptr, y, to_dt(y_dt), w4, false, plan, nullptr, nullptr, s};

@@ -402,21 +402,24 @@ inline int64_t expert_tiles(int64_t n_slots, int64_t n_experts, int64_t bm) {
     return n_slots / bm + (n_slots < n_experts ? n_slots : n_experts);
 }
 hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex);
-hipError_t launch_expert_down(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
-                              const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
-                              int n_mod, float* u, uint8_t* u_hl, const TileExtra& ex,
-                              hipStream_t s);
+// Stage 1 of the experts' layer with a compensation: the codes and scales of
+// x's rows, and u by slot (u_hl optional: rank <= 64).
+hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
+                                const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
+                                int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
+                                const TileExtra& ex, hipStream_t s);
 
 // Routing: at most kRouteMaxExperts experts and kRouteMaxK choices a token.
 // blocks == 0: one workgroup takes the batch and no workspace is needed.
 constexpr int kRouteMaxExperts = 512, kRouteMaxK = 16;
 struct RouteWs {
     int64_t blocks;
-    uint32_t* masks;      // [blocks][n_experts]
-    int32_t* before;      // [blocks][n_experts]
-    int32_t* totals;      // [n_experts]
+    uint32_t* masks;      // [blocks][route_pitch]
+    int32_t* before;      // [blocks][route_pitch] (many blocks only)
+    int32_t* totals;      // [route_pitch]
     size_t bytes;
 };
+inline int route_pitch(int n_experts) { return (n_experts + 3) / 4 * 4; }
 RouteWs plan_route(void* base, int64_t T, int E);
 hipError_t launch_route(const void* logits, DT dt, const int32_t* mod, int64_t T, int E, int k,
                         bool renorm, int32_t* experts, float* weights, int32_t* offsets,

@@ -4,10 +4,11 @@
 //                    residual: launch_gemm_tile_epilogue, launch_gemm_stream_epilogue
 //   k_route_*        the k largest logits of a token, their softmax weights, and
 //                    the choices of all tokens sorted by expert
-//   k_expert_down    u = (x S^-1) L1 of an expert's rows
+//   k_expert_stage1  u = (x S^-1) L1 of the experts' rows, beside the quantisation
 //   k_gemm_tile      (kTileExperts) the layer over rows sorted by expert
 //   k_combine        a token's expert rows, weighted and summed
 
+#include "masq_quant.h"
 #include "masq_tile.h"
 
 namespace masq {
@@ -19,20 +20,35 @@ hipError_t launch_tile_mode(const TileGemm& g, const TileExtra& ex, int tiles_m)
     const int bn = kTileShapes[g.plan.shape].bn;
     const int tiles_n = static_cast<int>((g.N + bn - 1) / bn);
     const int64_t nt = static_cast<int64_t>(tiles_m) * tiles_n * g.plan.S;
-#define MASQ_TILE(BM, BN, WM, WN, NST, WPE)                                                         \
-    hipLaunchKernelGGL((k_gemm_tile<YT, LT, CMC, false, W4, BM, BN, WM, WN, NST, WPE, MODE>),       \
-                       grid_of(8 * ((nt + 7) / 8), 64 * WM * WN), dim3(64 * WM * WN), 0, g.stream,  \
+#define MASQ_TILE_WK(BM, BN, WM, WN, NST, WPE, WK)                                                  \
+    hipLaunchKernelGGL((k_gemm_tile<YT, LT, CMC, false, W4, BM, BN, WM, WN, NST, WPE, MODE, WK>),   \
+                       grid_of(8 * ((nt + 7) / 8), 64 * WM * WN * WK), dim3(64 * WM * WN * WK), 0,  \
+                       g.stream,                                                                    \
                        g.q, g.wq, g.x_scale, g.w_scale, g.T, static_cast<int>(g.K),                 \
                        static_cast<int>(g.N), tiles_m, tiles_n, g.mod, g.u, g.u_hl, g.rank,         \
                        g.n_mod, static_cast<const LT*>(g.r_up), nullptr, static_cast<YT*>(g.y),     \
                        g.plan.S, g.part, g.tickets, g.a_pair, ex)
+#define MASQ_TILE(BM, BN, WM, WN, NST, WPE) MASQ_TILE_WK(BM, BN, WM, WN, NST, WPE, 1)
     switch (g.plan.shape) {
-        case 0: MASQ_TILE(32, 64, 1, 2, 3, 2); break;
+        case 0:
+            if constexpr (MODE == kTileExperts) {
+                // two waves a block, each half of a stage's columns; past 16
+                // stages a ring of four (us with one wave and three buffers / two
+                // and three / two and four: 16 tokens x 8 of 64 experts of 1024
+                // -> 2048 32.1 / 30.9 / 32.6, of 4096 -> 2048 130.3 / 124.0 / 110.9; one
+                // token 19.0 / 18.4 / 18.4)
+                if (g.K > 16 * kTileStageK) MASQ_TILE_WK(32, 64, 1, 2, 4, 2, 2);
+                else MASQ_TILE_WK(32, 64, 1, 2, 3, 2, 2);
+            } else {
+                MASQ_TILE(32, 64, 1, 2, 3, 2);
+            }
+            break;
         case 1: MASQ_TILE(64, 64, 2, 2, 3, 3); break;
         case 2: MASQ_TILE(128, 128, 2, 2, 2, 2); break;
         default: return hipErrorInvalidValue;
     }
 #undef MASQ_TILE
+#undef MASQ_TILE_WK
     return hipGetLastError();
 }
 
@@ -76,8 +92,10 @@ hipError_t launch_stream_epi(const StreamGemm& g, const TileExtra& ex) {
 // choice's place among the block's the count of the bits below its own.  So
 // slots ascend with the token inside an expert, whatever order anything ran in.
 constexpr int kRouteTokens = 32;
-constexpr int kRouteOneTokens = 256;      // at most this many: one workgroup does it all
+constexpr int kRouteOneTokens = 64;       // at most this many: one workgroup does it all
 constexpr int kRouteOneThreads = 1024;
+constexpr int kRouteChooseThreads = 1024;
+constexpr int64_t kRouteFewBlocks = 256;
 
 __device__ __forceinline__ uint32_t logit_key(float f) {
     if (!(f > -INFINITY)) return 0;                          // -inf, NaN
@@ -108,20 +126,23 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// Token t's choices by one wave: experts and weights to global memory, the
-// experts' mask bits to masks[expert].
+// The keys of token t (a wave; lane l: experts l, l + 64, ...).
 template <typename LT, int C>
-__device__ __forceinline__ void route_token(const LT* __restrict__ logits, int64_t t, int E, int k,
-                                            bool renorm, int32_t* __restrict__ experts,
-                                            float* __restrict__ weights, uint32_t* masks, int bit,
-                                            int lane) {
-    uint32_t key[C];
+__device__ __forceinline__ void load_keys(const LT* __restrict__ logits, int64_t t, int E, int lane,
+                                          uint32_t (&key)[C]) {
+    float f[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int e = lane + 64 * c;
-        const float f = Elem<LT>::load1(logits + t * E + min(e, E - 1));
-        key[c] = e < E ? logit_key(f) : 0;
-    }
+    for (int c = 0; c < C; ++c) f[c] = Elem<LT>::load1(logits + t * E + min(lane + 64 * c, E - 1));
+#pragma unroll
+    for (int c = 0; c < C; ++c) key[c] = lane + 64 * c < E ? logit_key(f[c]) : 0;
+}
+
+// A token's choices by one wave: experts and weights to global memory, the
+// experts' mask bits to masks[expert].
+template <int C>
+__device__ __forceinline__ void route_token(uint32_t (&key)[C], int k, bool renorm,
+                                            int32_t* __restrict__ experts, float* __restrict__ weights,
+                                            uint32_t* masks, int bit, int lane) {
     uint32_t all[C];                                         // as read (the rounds clear the chosen)
 #pragma unroll
     for (int c = 0; c < C; ++c) all[c] = key[c];
@@ -162,20 +183,38 @@ __device__ __forceinline__ void route_token(const LT* __restrict__ logits, int64
     }
     const float total = wave_sum(part);
     if (lane < k) {
-        experts[t * k + lane] = pick;
-        weights[t * k + lane] = pick >= 0 ? p / total : 0.f;
+        experts[lane] = pick;
+        weights[lane] = pick >= 0 ? p / total : 0.f;
         if (pick >= 0) atomicOr(&masks[pick], 1u << bit);
     }
 }
 
-template <typename LT>
-__device__ __forceinline__ void route_token_any(const LT* logits, int64_t t, int E, int k, bool renorm,
-                                                int32_t* experts, float* weights, uint32_t* masks,
-                                                int bit, int lane) {
-    if (E <= 64) route_token<LT, 1>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
-    else if (E <= 128) route_token<LT, 2>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
-    else if (E <= 256) route_token<LT, 4>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
-    else route_token<LT, 8>(logits, t, E, k, renorm, experts, weights, masks, bit, lane);
+// Tokens t0 + wave, + NW, ... of the n from t0 on, the next one's logits in
+// flight while one is chosen for; token i's bits go to masks row i / 32.
+template <typename LT, int C, int NW>
+__device__ __forceinline__ void route_tokens_c(const LT* logits, int64_t t0, int n, int E, int k,
+                                               bool renorm, int32_t* experts, float* weights,
+                                               uint32_t* masks, int pitch, int wave, int lane) {
+    uint32_t key[C], next[C];
+    if (wave < n) load_keys<LT, C>(logits, t0 + wave, E, lane, key);
+    for (int i = wave; i < n; i += NW) {                     // wave-uniform
+        load_keys<LT, C>(logits, t0 + min(i + NW, n - 1), E, lane, next);
+        route_token<C>(key, k, renorm, experts + (t0 + i) * k, weights + (t0 + i) * k,
+                       masks + (i >> 5) * pitch, i & 31, lane);
+#pragma unroll
+        for (int c = 0; c < C; ++c) key[c] = next[c];
+    }
+}
+template <typename LT, int NW>
+__device__ __forceinline__ void route_tokens(const LT* logits, int64_t t0, int n, int E, int k, bool renorm,
+                                             int32_t* experts, float* weights, uint32_t* masks, int pitch,
+                                             int wave, int lane) {
+#define MASQ_TOKENS(C) route_tokens_c<LT, C, NW>(logits, t0, n, E, k, renorm, experts, weights, masks, pitch, wave, lane)
+    if (E <= 64) MASQ_TOKENS(1);
+    else if (E <= 128) MASQ_TOKENS(2);
+    else if (E <= 256) MASQ_TOKENS(4);
+    else MASQ_TOKENS(8);
+#undef MASQ_TOKENS
 }
 
 // Exclusive prefix of v over the workgroup's first kRouteMaxExperts threads
@@ -216,8 +255,7 @@ __global__ __launch_bounds__(kRouteOneThreads) void k_route_one(
     const int words = (T + 31) >> 5;
     for (int i = tid; i < words * kRouteMaxExperts; i += kRouteOneThreads) (&masks[0][0])[i] = 0;
     __syncthreads();
-    for (int t = wave; t < T; t += NW)                       // wave-uniform
-        route_token_any<LT>(logits, t, E, k, renorm, experts, weights, masks[t >> 5], t & 31, lane);
+    route_tokens<LT, NW>(logits, 0, T, E, k, renorm, experts, weights, &masks[0][0], kRouteMaxExperts, wave, lane);
     __syncthreads();
     int cnt = 0, total;
     if (tid < E)
@@ -247,38 +285,42 @@ __global__ __launch_bounds__(kRouteOneThreads) void k_route_one(
     }
 }
 
-// Larger batches, in three launches: the choices and the masks of every 32
-// tokens, the masks' counts summed over the blocks before each, the places.
+// Larger batches: the choices and the masks of every 32 tokens, then their
+// places.  A workgroup of the second launch counts the choices of every expert
+// before its tokens and in all from the masks; where there are more than
+// kRouteFewBlocks of them, whose counting again in each would cost more than
+// another launch, a launch between the two leaves the sums.
 template <typename LT>
-__global__ __launch_bounds__(256) void k_route_choose(
+__global__ __launch_bounds__(kRouteChooseThreads) void k_route_choose(
     const LT* __restrict__ logits, int64_t T, int E, int k, bool renorm, int32_t* __restrict__ experts,
-    float* __restrict__ weights, uint32_t* __restrict__ masks) {
+    float* __restrict__ weights, uint32_t* __restrict__ masks, int pitch) {
     __shared__ uint32_t sm[kRouteMaxExperts];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int e = tid; e < E; e += 256) sm[e] = 0;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int e = tid; e < pitch; e += kRouteChooseThreads) sm[e] = 0;
     __syncthreads();
     const int64_t t0 = linear_block() * kRouteTokens;
     if (t0 >= T) return;
-    for (int i = wave; i < kRouteTokens && t0 + i < T; i += 4)
-        route_token_any<LT>(logits, t0 + i, E, k, renorm, experts, weights, sm, i, lane);
+    const int n = static_cast<int>(min(T - t0, static_cast<int64_t>(kRouteTokens)));
+    route_tokens<LT, kRouteChooseThreads / 64>(logits, t0, n, E, k, renorm, experts, weights, sm, 0, wave, lane);
     __syncthreads();
-    for (int e = tid; e < E; e += 256) masks[linear_block() * E + e] = sm[e];
+    for (int e = tid; e < pitch; e += kRouteChooseThreads) masks[linear_block() * pitch + e] = sm[e];
 }
 
 // A workgroup per 16 experts: 64 thread rows, each over a run of blocks.
 constexpr int kScanCols = 16, kScanRows = 64;
 __global__ __launch_bounds__(kScanCols * kScanRows) void k_route_scan(
-    const uint32_t* __restrict__ masks, int64_t blocks, int E, int32_t* __restrict__ before,
+    const uint32_t* __restrict__ masks, int64_t blocks, int pitch, int32_t* __restrict__ before,
     int32_t* __restrict__ totals) {
     __shared__ int part[kScanRows][kScanCols];
     const int col = threadIdx.x % kScanCols, row = threadIdx.x / kScanCols;
     const int e = blockIdx.x * kScanCols + col;
-    const bool in = e < E;
+    const bool in = e < pitch;
     const int64_t per = (blocks + kScanRows - 1) / kScanRows;
     const int64_t b0 = min(blocks, row * per), b1 = min(blocks, b0 + per);
     int sum = 0;
     if (in)
-        for (int64_t b = b0; b < b1; ++b) sum += __popc(masks[b * E + e]);
+        for (int64_t b = b0; b < b1; ++b) sum += __popc(masks[b * pitch + e]);
     part[row][col] = sum;
     __syncthreads();
     int at = 0, all = 0;
@@ -289,29 +331,60 @@ __global__ __launch_bounds__(kScanCols * kScanRows) void k_route_scan(
     }
     if (!in) return;
     for (int64_t b = b0; b < b1; ++b) {
-        before[b * E + e] = at;
-        at += __popc(masks[b * E + e]);
+        before[b * pitch + e] = at;
+        at += __popc(masks[b * pitch + e]);
     }
     if (row == 0) totals[e] = all;
 }
 
 __global__ __launch_bounds__(kRouteMaxExperts) void k_route_place(
     const int32_t* __restrict__ mod, int64_t T, int E, int k, const int32_t* __restrict__ experts,
-    const uint32_t* __restrict__ masks, const int32_t* __restrict__ before,
+    const uint32_t* __restrict__ masks, int pitch, int64_t blocks, const int32_t* __restrict__ before,
     const int32_t* __restrict__ totals, int32_t* __restrict__ offsets, int32_t* __restrict__ rows,
     int32_t* __restrict__ slots, int32_t* __restrict__ slot_mod) {
     constexpr int NT = kRouteMaxExperts;
     __shared__ int base[NT];
     __shared__ uint32_t sm[NT];
     __shared__ int waves[NT / 64];
+    __shared__ __attribute__((aligned(16))) v4i sums[2][NT];
     const int tid = threadIdx.x;
     const int64_t b = linear_block(), t0 = b * kRouteTokens;
     if (t0 >= T) return;
+    int mine = 0, all = 0;                                   // of expert tid: before this block, in all
+    if (before != nullptr) {
+        if (tid < E) {
+            mine = before[b * pitch + tid];
+            all = totals[tid];
+        }
+    } else {
+        // thread (row, 4 experts): every rows-th block's masks
+        const int quads = pitch >> 2, rows_ = NT / quads, row = tid / quads, qd = tid - row * quads;
+        v4i lo = {0, 0, 0, 0}, sum = {0, 0, 0, 0};
+        if (row < rows_) {
+#pragma unroll 8
+            for (int i = row; i < static_cast<int>(blocks); i += rows_) {
+                const v4i w = *reinterpret_cast<const v4i*>(masks + static_cast<int64_t>(i) * pitch + 4 * qd);
+                v4i c;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[j] = static_cast<int>(__popc(static_cast<uint32_t>(w[j])));
+                sum += c;
+                if (i < b) lo += c;
+            }
+        }
+        sums[0][tid] = lo;
+        sums[1][tid] = sum;
+        __syncthreads();
+        if (tid < E)
+            for (int g = 0; g < rows_; ++g) {
+                mine += sums[0][g * quads + (tid >> 2)][tid & 3];
+                all += sums[1][g * quads + (tid >> 2)][tid & 3];
+            }
+    }
     int total;
-    const int first = expert_prefix<NT>(tid < E ? totals[tid] : 0, waves, &total, tid);
+    const int first = expert_prefix<NT>(all, waves, &total, tid);
     if (tid < E) {
-        base[tid] = first + before[b * E + tid];
-        sm[tid] = masks[b * E + tid];
+        base[tid] = first + mine;
+        sm[tid] = masks[b * pitch + tid];
         if (b == 0) offsets[tid] = first;
     }
     if (b == 0 && tid == 0) offsets[E] = total;
@@ -334,55 +407,55 @@ __global__ __launch_bounds__(kRouteMaxExperts) void k_route_place(
     }
 }
 
-// ================================================================ experts' down-projection
-// u[slot] = (x S_m^-1) L1_e^m for the slots of modality m != text: a workgroup
-// takes 32 slots of one expert and 64 columns of the rank, its eight waves an
-// eighth of the row each, and the waves' sums are added in their order.  With
-// bf16 factors the smoothed row enters as a hi + lo pair of bf16 terms, as in
-// the layer; with fp32 factors the fp32 MFMA takes it whole.  Each modality is
-// summed on its own, so that an infinite factor stays with its modality.
-constexpr int kEdSlots = 32, kEdWaves = 8, kEdRank = 64;
+// ================================================================ stage 1 of the experts' layer
+// One launch for two independent pieces of work: workgroups below `downs` form
+// u = (x S_m^-1) L1_e^m for the slots of modality m != text, those past them
+// quantise x's rows (a row a workgroup for small batches, where a row's latency
+// counts, else a row a wave).
+//
+// A down-projection workgroup takes 16 RG slots of one expert and 16 RB columns
+// of the rank, its eight waves an eighth of the row each, U steps of 32 columns
+// in flight, and the waves' sums are added in their order.  With bf16 factors
+// the smoothed row enters as a hi + lo pair of bf16 terms, as in the layer;
+// with fp32 factors the fp32 MFMA takes it whole.  Each modality is summed on
+// its own, so that an infinite factor stays with its modality.
+constexpr int kEdWaves = 8;
 
-template <typename XT, typename LT>
-__global__ __launch_bounds__(64 * kEdWaves) void k_expert_down(
-    const XT* __restrict__ x, const int32_t* __restrict__ mod, const float* __restrict__ inv_s,
-    const LT* __restrict__ l_down, int64_t n_slots, int K, int r, int n_mod, float* __restrict__ u,
-    uint8_t* __restrict__ u_hl, TileExtra ex) {
-    constexpr int RG = kEdSlots / 16, RB = kEdRank / 16;
-    static_assert(RG * RB * 64 == 64 * kEdWaves, "a thread finishes one 16-byte piece of u");
-    __shared__ __attribute__((aligned(16))) v4f red[kEdWaves][RG * RB * 64];
+struct ExpertStage1 {
+    const int32_t* mod;
+    const float* inv_s;
+    int64_t n_slots, T;
+    int K, r, n_mod;
+    float* u;
+    uint8_t* u_hl;
+    int8_t* q;
+    float* x_scale;
+    int64_t downs;
+    bool row_group;       // a row a workgroup
+};
+
+template <typename XT, typename LT, int RG, int RB, int U>
+__device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const LT* __restrict__ l_down,
+                                                 const ExpertStage1& a, const TileExtra& ex,
+                                                 v4f (&red)[kEdWaves][RG * RB * 64]) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int K = a.K, r = a.r;
     GroupTile gt;
-    if (!group_tile<kEdSlots>(ex, n_slots, linear_block(), (r + kEdRank - 1) / kEdRank, gt)) return;
-    const int c0 = gt.tn * kEdRank;
+    if (!group_tile<16 * RG>(ex, a.n_slots, linear_block(), (r + 16 * RB - 1) / (16 * RB), gt)) return;
+    const int c0 = gt.tn * 16 * RB;
     const int nb = min(RB, (r - c0) >> 4);                   // 16-column blocks of the rank
     const int steps = (K + 31) >> 5, per = (steps + kEdWaves - 1) / kEdWaves;
     const int st0 = wave * per, st1 = min(steps, st0 + per);
     const XT* xp[RG];
-    const float* ip[RG];
     int md[RG];
 #pragma unroll
     for (int g = 0; g < RG; ++g) {
         const int64_t ar = slot_row(ex, min(gt.first + 16 * g + (lane & 15), gt.end - 1));
-        md[g] = sane_mod(mod[ar], n_mod);
+        md[g] = sane_mod(a.mod[ar], a.n_mod);
         xp[g] = x + ar * K;
-        ip[g] = inv_s + static_cast<int64_t>(md[g]) * K;
     }
-    // thread tid finishes block (og, ob): columns 4 (lane / 16) .. of slot lane % 16
-    const int og = wave / RB, ob = wave % RB;
-    const int64_t slot = gt.first + 16 * og + (lane & 15);
-    const int omd = og == 0 ? md[0] : md[RG - 1];
-    const bool store = ob < nb && slot < gt.end;
-    auto put_hl = [&](v4f v) __attribute__((always_inline)) {
-        uint8_t* p = u_hl + slot * 256 + 2 * (16 * ob + 4 * (lane >> 4));
-        const uint32_t h0 = pack_bf16x2(v.x, v.y), h1 = pack_bf16x2(v.z, v.w);
-        *reinterpret_cast<v2i*>(p) = v2i{static_cast<int32_t>(h0), static_cast<int32_t>(h1)};
-        *reinterpret_cast<v2i*>(p + 128) =
-            v2i{static_cast<int32_t>(pack_bf16x2(v.x - __uint_as_float(h0 << 16), v.y - __uint_as_float(h0 & 0xFFFF0000u))),
-                static_cast<int32_t>(pack_bf16x2(v.z - __uint_as_float(h1 << 16), v.w - __uint_as_float(h1 & 0xFFFF0000u)))};
-    };
-    for (int m = 1; m < n_mod; ++m) {
+    for (int m = 1; m < a.n_mod; ++m) {
         bool live[RG], any = false;
 #pragma unroll
         for (int g = 0; g < RG; ++g) {
@@ -390,52 +463,70 @@ __global__ __launch_bounds__(64 * kEdWaves) void k_expert_down(
             any = any || live[g];
         }
         if (__ballot(any) == 0ull) continue;                 // uniform over the workgroup: same rows
-        const LT* lm = l_down + (static_cast<int64_t>(gt.expert) * (n_mod - 1) + m - 1) * r * K;
+        const LT* lm = l_down + (static_cast<int64_t>(gt.expert) * (a.n_mod - 1) + m - 1) * r * K;
+        const float* im = a.inv_s + static_cast<int64_t>(m) * K;
         v4f acc[RG][RB];
 #pragma unroll
         for (int g = 0; g < RG; ++g)
 #pragma unroll
             for (int b = 0; b < RB; ++b) acc[g][b] = v4f{0.f, 0.f, 0.f, 0.f};
-        for (int st = st0; st < st1; ++st) {
-            const int k = 32 * st + 8 * (lane >> 4);
-            const bool in = k < K;                           // K % 16 == 0: 8 columns in or out together
-            const int kc = min(k, K - 8);
-            Raw8<LT> lv[RB];
+        for (int s0 = st0; s0 < st1; s0 += U) {
+            Raw8<LT> lv[U][RB];
+            Raw8<XT> xv[U][RG];
+            Raw8<float> sv[U];
+            bool in[U];
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
-                lv[b].load(lm + static_cast<int64_t>(c0 + 16 * min(b, nb - 1) + (lane & 15)) * K + kc);
-            float xs[RG][8];
+            for (int i = 0; i < U; ++i) {
+                const int k = 32 * (s0 + i) + 8 * (lane >> 4);
+                in[i] = s0 + i < st1 && k < K;               // K % 16 == 0: 8 columns in or out together
+                const int kc = min(k, K - 8);
 #pragma unroll
-            for (int g = 0; g < RG; ++g) {
-                float f[8], s[8];
-                Elem<XT>::load8(xp[g] + kc, f);
-                load8_f32(ip[g] + kc, s);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) xs[g][e] = live[g] && in ? f[e] * s[e] : 0.f;
+                for (int b = 0; b < RB; ++b)
+                    lv[i][b].load(lm + static_cast<int64_t>(c0 + 16 * min(b, nb - 1) + (lane & 15)) * K + kc);
+                sv[i].load(im + kc);
             }
-            if constexpr (sizeof(LT) == 2) {
-                const v4i zero = {0, 0, 0, 0};
+#pragma unroll
+            for (int g = 0; g < RG; ++g)                     // (the others' lanes ask for nothing)
+                if (live[g]) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+                        xv[i][g].load(xp[g] + min(32 * (s0 + i) + 8 * (lane >> 4), K - 8));
+                }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                float sm[8];
+                sv[i].to_f32(sm);
+                float xs[RG][8];
 #pragma unroll
                 for (int g = 0; g < RG; ++g) {
-                    v4i hi, lo;
-                    split_bf16x8(xs[g], hi, lo);
+                    xv[i][g].to_f32(xs[g]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) xs[g][e] = live[g] && in[i] ? xs[g][e] * sm[e] : 0.f;
+                }
+                if constexpr (sizeof(LT) == 2) {
+                    const v4i zero = {0, 0, 0, 0};
+#pragma unroll
+                    for (int g = 0; g < RG; ++g) {
+                        v4i hi, lo;
+                        split_bf16x8(xs[g], hi, lo);
+#pragma unroll
+                        for (int b = 0; b < RB; ++b) {
+                            const v8bf w = __builtin_bit_cast(v8bf, in[i] ? lv[i][b].a : zero);
+                            acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, hi), acc[g][b], 0, 0, 0);
+                            acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, lo), acc[g][b], 0, 0, 0);
+                        }
+                    }
+                } else {
 #pragma unroll
                     for (int b = 0; b < RB; ++b) {
-                        const v8bf w = __builtin_bit_cast(v8bf, in ? lv[b].a : zero);
-                        acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, hi), acc[g][b], 0, 0, 0);
-                        acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, lo), acc[g][b], 0, 0, 0);
+                        float w[8];
+                        lv[i][b].to_f32(w);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+#pragma unroll
+                            for (int g = 0; g < RG; ++g)
+                                acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in[i] ? w[e] : 0.f, xs[g][e], acc[g][b], 0, 0, 0);
                     }
-                }
-            } else {
-#pragma unroll
-                for (int b = 0; b < RB; ++b) {
-                    float w[8];
-                    lv[b].to_f32(w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int g = 0; g < RG; ++g)
-                            acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? w[e] : 0.f, xs[g][e], acc[g][b], 0, 0, 0);
                 }
             }
         }
@@ -444,14 +535,47 @@ __global__ __launch_bounds__(64 * kEdWaves) void k_expert_down(
 #pragma unroll
             for (int b = 0; b < RB; ++b) red[wave][(g * RB + b) * 64 + lane] = acc[g][b];
         __syncthreads();
-        v4f v = red[0][tid];
+        // item 64 (RB g + b) + lane: columns 4 (lane / 16) .. of slot lane % 16
 #pragma unroll
-        for (int w = 1; w < kEdWaves; ++w) v = v + red[w][tid];
-        if (store && omd == m) {
-            *reinterpret_cast<v4f*>(u + slot * r + c0 + 16 * ob + 4 * (lane >> 4)) = v;
-            if (u_hl != nullptr) put_hl(v);
+        for (int it = wave; it < RG * RB; it += kEdWaves) {
+            const int g = it / RB, b = it % RB;
+            v4f v = red[0][it * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < kEdWaves; ++w) v = v + red[w][it * 64 + lane];
+            const int64_t slot = gt.first + 16 * g + (lane & 15);
+            bool mine = false;
+#pragma unroll
+            for (int g2 = 0; g2 < RG; ++g2) mine = mine || (g2 == g && live[g2]);
+            if (b >= nb || slot >= gt.end || !mine) continue;
+            const int c = c0 + 16 * b + 4 * (lane >> 4);
+            *reinterpret_cast<v4f*>(a.u + slot * r + c) = v;
+            if (a.u_hl == nullptr) continue;                 // rank <= 64: also as bf16 hi | lo
+            uint8_t* p = a.u_hl + slot * 256 + 2 * c;
+            const uint32_t h0 = pack_bf16x2(v.x, v.y), h1 = pack_bf16x2(v.z, v.w);
+            const uint32_t l0 = pack_bf16x2(v.x - __uint_as_float(h0 << 16), v.y - __uint_as_float(h0 & 0xFFFF0000u));
+            const uint32_t l1 = pack_bf16x2(v.z - __uint_as_float(h1 << 16), v.w - __uint_as_float(h1 & 0xFFFF0000u));
+            *reinterpret_cast<v2i*>(p) = v2i{static_cast<int32_t>(h0), static_cast<int32_t>(h1)};
+            *reinterpret_cast<v2i*>(p + 128) = v2i{static_cast<int32_t>(l0), static_cast<int32_t>(l1)};
         }
         __syncthreads();                                     // red is free for the next modality
+    }
+}
+
+template <typename XT, typename LT, int RG, int RB, int U>
+__global__ __launch_bounds__(64 * kEdWaves, 4) void k_expert_stage1(const XT* __restrict__ x,
+                                                                 const LT* __restrict__ l_down,
+                                                                 ExpertStage1 a, TileExtra ex) {
+    __shared__ __attribute__((aligned(16))) v4f red[kEdWaves][RG * RB * 64];
+    const int64_t b = linear_block() - a.downs;
+    if (b < 0) {
+        expert_down_tile<XT, LT, RG, RB, U>(x, l_down, a, ex, red);
+    } else if (a.row_group) {
+        if (b < a.T) sq_row<XT, 64 * kEdWaves, 2>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, b, false);
+    } else {
+        const int64_t t = b * kEdWaves + (threadIdx.x >> 6);
+        if (t < a.T)
+            quant_row_wave<XT, 4>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, t, false, threadIdx.x & 63,
+                                  [](int) {});
     }
 }
 
@@ -531,25 +655,43 @@ hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex) {
         g, ex, static_cast<int>(expert_tiles(g.T, ex.n_experts, kTileShapes[g.plan.shape].bm)));
 }
 
-hipError_t launch_expert_down(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
-                              const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
-                              int n_mod, float* u, uint8_t* u_hl, const TileExtra& ex,
-                              hipStream_t s) {
-    const int64_t nt = expert_tiles(n_slots, ex.n_experts, kEdSlots) * ((rank + kEdRank - 1) / kEdRank);
-    const dim3 grid = grid_of(8 * ((nt + 7) / 8), 64 * kEdWaves), block(64 * kEdWaves);
-#define MASQ_DOWN(XT, LT)                                                                           \
-    hipLaunchKernelGGL((k_expert_down<XT, LT>), grid, block, 0, s, static_cast<const XT*>(x), mod,  \
-                       inv_s, static_cast<const LT*>(l_down), n_slots, static_cast<int>(K), rank,   \
-                       n_mod, u, u_hl, ex)
-    if (x_dt == DT::BF16) {
-        if (lr_dt == DT::BF16) MASQ_DOWN(bf16_t, bf16_t);
-        else MASQ_DOWN(bf16_t, float);
-    } else {
-        if (lr_dt == DT::BF16) MASQ_DOWN(float, bf16_t);
-        else MASQ_DOWN(float, float);
-    }
-#undef MASQ_DOWN
+// Slots of a down-projection workgroup: 16 while that makes at most two
+// workgroups a compute unit, 32 up to four, else 64 where the rank leaves the
+// registers for it (L1 is read once a workgroup).
+template <typename XT, typename LT, int RB>
+static hipError_t launch_stage1_t(const void* x, const void* l_down, ExpertStage1 a, const TileExtra& ex,
+                                  hipStream_t s) {
+    const int64_t quant = a.row_group ? a.T : (a.T + kEdWaves - 1) / kEdWaves;
+    const int chunks = (a.r + 16 * RB - 1) / (16 * RB);
+    const int64_t most = expert_tiles(a.n_slots, ex.n_experts, 16) * chunks;
+#define MASQ_STAGE1(RG, U)                                                                          \
+    do {                                                                                            \
+        a.downs = 8 * ((expert_tiles(a.n_slots, ex.n_experts, 16 * RG) * chunks + 7) / 8);          \
+        hipLaunchKernelGGL((k_expert_stage1<XT, LT, RG, RB, U>), grid_of(a.downs + quant, 64 * kEdWaves), \
+                           dim3(64 * kEdWaves), 0, s, static_cast<const XT*>(x),                    \
+                           static_cast<const LT*>(l_down), a, ex);                                  \
+    } while (0)
+    constexpr bool kNarrow = sizeof(XT) == 2 && sizeof(LT) == 2;
+    if (most <= 512) MASQ_STAGE1(1, (kNarrow ? 4 : 2));
+    else if (most <= 1024 || RB > 2) MASQ_STAGE1(2, 2);
+    else MASQ_STAGE1((RB > 2 ? 2 : 4), 2);
+#undef MASQ_STAGE1
     return hipGetLastError();
+}
+
+hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
+                                const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
+                                int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
+                                const TileExtra& ex, hipStream_t s) {
+    ExpertStage1 a{mod, inv_s, n_slots, T, static_cast<int>(K), rank, n_mod, u, u_hl, q, x_scale, 0,
+                   T < kRowsPerWaveMinT};
+#define MASQ_RB(XT, LT)                                                                             \
+    (rank <= 16 ? launch_stage1_t<XT, LT, 1>(x, l_down, a, ex, s)                                   \
+                : (rank <= 32 ? launch_stage1_t<XT, LT, 2>(x, l_down, a, ex, s)                     \
+                              : launch_stage1_t<XT, LT, 4>(x, l_down, a, ex, s)))
+    if (x_dt == DT::BF16) return lr_dt == DT::BF16 ? MASQ_RB(bf16_t, bf16_t) : MASQ_RB(bf16_t, float);
+    return lr_dt == DT::BF16 ? MASQ_RB(float, bf16_t) : MASQ_RB(float, float);
+#undef MASQ_RB
 }
 
 hipError_t launch_route(const void* logits, DT dt, const int32_t* mod, int64_t T, int E, int k,
@@ -566,17 +708,20 @@ hipError_t launch_route(const void* logits, DT dt, const int32_t* mod, int64_t T
 #undef MASQ_ROUTE
         return hipGetLastError();
     }
-    const dim3 grid = grid_of(w.blocks, 256);
+    const int pitch = route_pitch(E);
+    const dim3 grid = grid_of(w.blocks, kRouteChooseThreads);
 #define MASQ_ROUTE(LT)                                                                              \
-    hipLaunchKernelGGL(k_route_choose<LT>, grid, dim3(256), 0, s, static_cast<const LT*>(logits),   \
-                       T, E, k, renorm, experts, weights, w.masks)
+    hipLaunchKernelGGL(k_route_choose<LT>, grid, dim3(kRouteChooseThreads), 0, s,                   \
+                       static_cast<const LT*>(logits), T, E, k, renorm, experts, weights, w.masks, pitch)
     if (dt == DT::BF16) MASQ_ROUTE(bf16_t);
     else MASQ_ROUTE(float);
 #undef MASQ_ROUTE
-    hipLaunchKernelGGL(k_route_scan, dim3(static_cast<unsigned>((E + kScanCols - 1) / kScanCols)),
-                       dim3(kScanCols * kScanRows), 0, s, w.masks, w.blocks, E, w.before, w.totals);
+    if (w.before != nullptr)
+        hipLaunchKernelGGL(k_route_scan, dim3(static_cast<unsigned>((pitch + kScanCols - 1) / kScanCols)),
+                           dim3(kScanCols * kScanRows), 0, s, w.masks, w.blocks, pitch, w.before, w.totals);
     hipLaunchKernelGGL(k_route_place, grid_of(w.blocks, kRouteMaxExperts), dim3(kRouteMaxExperts), 0, s,
-                       mod, T, E, k, experts, w.masks, w.before, w.totals, offsets, rows, slots, slot_mod);
+                       mod, T, E, k, experts, w.masks, pitch, w.blocks, w.before, w.totals, offsets, rows,
+                       slots, slot_mod);
     return hipGetLastError();
 }
 
@@ -584,14 +729,17 @@ RouteWs plan_route(void* base, int64_t T, int E) {
     RouteWs w{};
     if (T <= kRouteOneTokens) return w;
     w.blocks = (T + kRouteTokens - 1) / kRouteTokens;
-    const size_t table = (static_cast<size_t>(w.blocks) * E * 4 + 255) / 256 * 256;
+    const size_t table = (static_cast<size_t>(w.blocks) * route_pitch(E) * 4 + 255) / 256 * 256;
+    const bool scan = w.blocks > kRouteFewBlocks;
     uint8_t* b = static_cast<uint8_t*>(base);
     if (b != nullptr) {
         w.masks = reinterpret_cast<uint32_t*>(b);
-        w.before = reinterpret_cast<int32_t*>(b + table);
-        w.totals = reinterpret_cast<int32_t*>(b + 2 * table);
+        if (scan) {
+            w.before = reinterpret_cast<int32_t*>(b + table);
+            w.totals = reinterpret_cast<int32_t*>(b + 2 * table);
+        }
     }
-    w.bytes = 2 * table + (static_cast<size_t>(E) * 4 + 255) / 256 * 256;
+    w.bytes = scan ? 2 * table + (static_cast<size_t>(route_pitch(E)) * 4 + 255) / 256 * 256 : table;
     return w;
 }
 

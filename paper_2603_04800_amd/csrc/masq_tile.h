@@ -139,15 +139,15 @@ __device__ __forceinline__ int ts_swz4(int row) { return (row >> 2) & 3; }
 constexpr int ts_stage_bytes(int bm, int bn, bool w4) { return bm * kTsK + bn * (w4 ? kTsK / 2 : kTsK); }
 
 template <typename YT, typename LT, bool CMC, bool ACC, bool W4, int BM, int BN, int WM, int WN,
-          int NST, int WPE, int MODE = kTilePlain>
-__global__ __launch_bounds__(64 * WM * WN, WPE) void k_gemm_tile(
+          int NST, int WPE, int MODE = kTilePlain, int WK = 1>
+__global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
     const int8_t* __restrict__ A, const int8_t* __restrict__ B, const float* __restrict__ x_scale,
     const float* __restrict__ w_scale, int64_t T, int K, int N, int tiles_m, int tiles_n,
     const int32_t* __restrict__ mod, const float* __restrict__ u, const uint8_t* __restrict__ u_hl,
     int r, int n_mod, const LT* __restrict__ r_up, int32_t* __restrict__ acc_out,
     YT* __restrict__ y, int S, int32_t* __restrict__ part, int* __restrict__ tickets, bool a_pair, TileExtra ex) {
     constexpr bool GRP = MODE == kTileExperts;
-    constexpr int NW = WM * WN, NT = 64 * NW;
+    constexpr int NW = WM * WN * WK, NT = 64 * NW;
     constexpr int MI = BM / WM / 32, NJ = BN / WN / 32;     // 32 x 32 blocks of a wave
     constexpr int kRowB = W4 ? kTsK / 2 : kTsK;             // B bytes per row and stage
     constexpr int kStage = ts_stage_bytes(BM, BN, W4);
@@ -161,7 +161,9 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void k_gemm_tile(
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / WN, wn = wave % WN;
+    // (WK: waves that share a block take WK-ths of a stage's columns each)
+    const int wm = wave / WN % WM, wn = wave % WN, wk = wave / (WM * WN);
+    static_assert(WK == 1 || (GRP && WM == 1 && 4 % WK == 0), "shared blocks: the experts' small tiles");
     int tm, tn;
     // output rows [row0, rend) of the tile; GRP: slots of expert `expert`
     int64_t row0, rend = T;
@@ -263,11 +265,49 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void k_gemm_tile(
 
     // one stage: 4 steps of 32 k.  Lane group h = lane / 32 takes 16-byte
     // piece 2 ks + h of the rows (W4: the 8 packed bytes of the same codes).
-    auto compute = [&](int buf, int valid) __attribute__((always_inline)) {   // valid: pieces within K
+    auto compute = [&](int buf, int valid, auto between) __attribute__((always_inline)) {   // valid: pieces within K
         const uint8_t* sa = ring + buf * kStage;
         const uint8_t* sb = sa + BM * kTsK;
         const int h = lane >> 5;
         const v4i zero = {0, 0, 0, 0};
+        if constexpr (GRP) {
+            // every fragment of the stage is read before `between` (the next
+            // stage's DMA), whose issue hides the reads' latency
+            constexpr int kN = 4 / WK;
+            v4i ga[kN][MI];
+            std::conditional_t<W4, v2i, v4i> gb[kN][NJ];
+#pragma unroll
+            for (int s = 0; s < kN; ++s) {
+                const int ks = WK == 1 ? s : kN * wk + s;
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const int row = wm * (BM / WM) + 32 * i + (lane & 31);
+                    ga[s][i] = *reinterpret_cast<const v4i*>(sa + row * kTsK + (((2 * ks + h) ^ ts_swz(row)) << 4));
+                    if (valid < 8) ga[s][i] = 2 * ks + h < valid ? ga[s][i] : zero;
+                }
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const int row = wn * (BN / WN) + 32 * j + (lane & 31);
+                    if constexpr (W4)
+                        gb[s][j] = *reinterpret_cast<const v2i*>(sb + row * kRowB + ((ks ^ ts_swz4(row)) << 4) + 8 * h);
+                    else
+                        gb[s][j] = *reinterpret_cast<const v4i*>(sb + row * kRowB + (((2 * ks + h) ^ ts_swz(row)) << 4));
+                }
+            }
+            between();
+#pragma unroll
+            for (int s = 0; s < kN; ++s)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    v4i b;
+                    if constexpr (W4) b = w4_operand(gb[s][j]);
+                    else b = gb[s][j];
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b, ga[s][i], acc[i][j], 0, 0, 0);
+                }
+            return;
+        }
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             v4i fa[MI], fb[NJ];
@@ -309,18 +349,50 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void k_gemm_tile(
 
     for (int st = 0; st < NST - 1 && st < ns; ++st) issue(st, st);
     int st = 0, cur = 0, nxt = NST - 1;                     // stage, its buffer, the one to refill
+    // (GRP) the tile ends above this wave's rows: its loads and barriers only
+    const bool idle = GRP && row0 + wm * (BM / WM) >= rend;
     for (; st + NST - 1 < ns; ++st) {
         publish(NST - 2);
-        issue(st + NST - 1, nxt);
-        compute(cur, 8);
+        auto refill = [&]() __attribute__((always_inline)) { issue(st + NST - 1, nxt); };
+        if constexpr (GRP) {
+            if (idle) refill();
+            else compute(cur, 8, refill);
+        } else {
+            refill();
+            compute(cur, 8, [] {});
+        }
         cur = cur + 1 == NST ? 0 : cur + 1;
         nxt = nxt + 1 == NST ? 0 : nxt + 1;
     }
     for (; st < ns; ++st) {
         publish(min(ns - 1 - st, NST - 2));
-        if (s0 + st == nst_all - 1 && rem < kTsK) compute(cur, rem >> 4);
-        else compute(cur, 8);
+        if (idle) continue;
+        if (s0 + st == nst_all - 1 && rem < kTsK) compute(cur, rem >> 4, [] {});
+        else compute(cur, 8, [] {});
         cur = cur + 1 == NST ? 0 : cur + 1;
+    }
+    if constexpr (WK > 1) {
+        // the sharers' sums are added through LDS, exactly; the first of them
+        // finishes the block
+        static_assert(MI == 1 && NJ == 1 && NST * kStage >= (WK - 1) * WN * 4096, "one block a wave");
+        v4i* part = reinterpret_cast<v4i*>(ring) + wn * 256 + lane;
+        __syncthreads();
+        if (wk > 0) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                part[(wk - 1) * WN * 256 + 64 * g] = v4i{acc[0][0][4 * g], acc[0][0][4 * g + 1], acc[0][0][4 * g + 2],
+                                                         acc[0][0][4 * g + 3]};
+        }
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int k = 0; k < WK - 1; ++k)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const v4i v = part[k * WN * 256 + 64 * g];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[0][0][4 * g + e] += v[e];
+            }
     }
     if constexpr (W4) {
 #pragma unroll
@@ -418,7 +490,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void k_gemm_tile(
         float* scr = reinterpret_cast<float*>(ring) + wave * 32 * kEpiPitch;
         const float* bias = ex.bias != nullptr ? ex.bias + static_cast<int64_t>(expert) * N : nullptr;
 #pragma unroll 1
-        for (int i = 0; i < MI; ++i) {                      // (the blocks move down a row a turn)
+        for (int i = 0; i < MI && trow + 32 * i < rend; ++i) {   // (the blocks move down a row a turn)
             finish_row<YT, NJ>(yb[0], ex, bias, scr, y, trow + 32 * i, rend, tcol, N, lane);
 #pragma unroll
             for (int k = 0; k + 1 < MI; ++k)

@@ -150,7 +150,8 @@ def _check_route(ops, logits, k, renorm, mod=None):
 
 
 @pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 2, 1), (1, 64, 8), (4, 64, 8), (31, 10, 3), (33, 65, 16),
-                                   (256, 128, 8), (257, 128, 8), (300, 512, 16), (1000, 7, 7), (2049, 60, 4)])
+                                   (256, 128, 8), (257, 128, 8), (300, 512, 16), (64, 9, 2), (65, 510, 3), (1000, 7, 7), (2049, 60, 4),
+                                   (8192, 6, 2), (8225, 13, 2)])
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_route(ops, T, E, k, io):
     g = _gen(T + E)
