@@ -434,10 +434,15 @@ struct ExpertStage1 {
     bool row_group;       // a row a workgroup
 };
 
+// The tile's slots of one modality come side by side first (a list in LDS), so
+// that a group of 16 MFMA columns holds slots that count: a tile of which half
+// is text costs half the loads and products.  A column's sums depend on its own
+// row only, so the columns past the last slot may hold anything.
 template <typename XT, typename LT, int RG, int RB, int U>
 __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const LT* __restrict__ l_down,
                                                  const ExpertStage1& a, const TileExtra& ex,
-                                                 v4f (&red)[kEdWaves][RG * RB * 64]) {
+                                                 v4f (&red)[kEdWaves][RG * RB * 64], int (&list)[64]) {
+    static_assert(RG <= 4, "a lane per slot");
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int K = a.K, r = a.r;
@@ -447,106 +452,100 @@ __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const
     const int nb = min(RB, (r - c0) >> 4);                   // 16-column blocks of the rank
     const int steps = (K + 31) >> 5, per = (steps + kEdWaves - 1) / kEdWaves;
     const int st0 = wave * per, st1 = min(steps, st0 + per);
-    const XT* xp[RG];
-    int md[RG];
-#pragma unroll
-    for (int g = 0; g < RG; ++g) {
-        const int64_t ar = slot_row(ex, min(gt.first + 16 * g + (lane & 15), gt.end - 1));
-        md[g] = sane_mod(a.mod[ar], a.n_mod);
-        xp[g] = x + ar * K;
-    }
+    const int count = static_cast<int>(gt.end - gt.first);
+    // lane l: slot l of the tile
+    const int row_l = static_cast<int>(slot_row(ex, min(gt.first + lane, gt.end - 1)));
+    const int md_l = lane < count ? sane_mod(a.mod[row_l], a.n_mod) : 0;
     for (int m = 1; m < a.n_mod; ++m) {
-        bool live[RG], any = false;
-#pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            live[g] = md[g] == m;
-            any = any || live[g];
-        }
-        if (__ballot(any) == 0ull) continue;                 // uniform over the workgroup: same rows
+        const unsigned long long mask = __ballot(md_l == m);
+        if (mask == 0ull) continue;                          // the same in every wave
+        const int n = __builtin_popcountll(mask);
+        if (wave == 0 && md_l == m) list[__builtin_popcountll(mask & ((1ull << lane) - 1ull))] = lane;
+        __syncthreads();
         const LT* lm = l_down + (static_cast<int64_t>(gt.expert) * (a.n_mod - 1) + m - 1) * r * K;
         const float* im = a.inv_s + static_cast<int64_t>(m) * K;
+        const XT* xp[RG];
+#pragma unroll
+        for (int g = 0; g < RG; ++g)                         // (places past n repeat the last slot)
+            xp[g] = x + static_cast<int64_t>(__shfl(row_l, list[min(16 * g + (lane & 15), n - 1)])) * K;
         v4f acc[RG][RB];
 #pragma unroll
         for (int g = 0; g < RG; ++g)
 #pragma unroll
             for (int b = 0; b < RB; ++b) acc[g][b] = v4f{0.f, 0.f, 0.f, 0.f};
-        for (int s0 = st0; s0 < st1; s0 += U) {
-            Raw8<LT> lv[U][RB];
-            Raw8<XT> xv[U][RG];
-            Raw8<float> sv[U];
-            bool in[U];
+        // CNT steps from s0 on; TAIL: the last ones, which may end inside a step
+        auto run = [&](int s0, auto cnt, auto tail) __attribute__((always_inline)) {
+            constexpr int CNT = decltype(cnt)::value;
+            constexpr bool TAIL = decltype(tail)::value;
+            Raw8<LT> lv[CNT][RB];
+            Raw8<XT> xv[CNT][RG];
+            Raw8<float> sv[CNT];
+            bool in[CNT];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
+            for (int i = 0; i < CNT; ++i) {
                 const int k = 32 * (s0 + i) + 8 * (lane >> 4);
-                in[i] = s0 + i < st1 && k < K;               // K % 16 == 0: 8 columns in or out together
-                const int kc = min(k, K - 8);
+                in[i] = !TAIL || k < K;                      // K % 16 == 0: 8 columns in or out together
+                const int kc = TAIL ? min(k, K - 8) : k;
 #pragma unroll
                 for (int b = 0; b < RB; ++b)
                     lv[i][b].load(lm + static_cast<int64_t>(c0 + 16 * min(b, nb - 1) + (lane & 15)) * K + kc);
                 sv[i].load(im + kc);
+#pragma unroll
+                for (int g = 0; g < RG; ++g)
+                    if (16 * g < n) xv[i][g].load(xp[g] + kc);               // uniform
             }
 #pragma unroll
-            for (int g = 0; g < RG; ++g)                     // (the others' lanes ask for nothing)
-                if (live[g]) {
-#pragma unroll
-                    for (int i = 0; i < U; ++i)
-                        xv[i][g].load(xp[g] + min(32 * (s0 + i) + 8 * (lane >> 4), K - 8));
-                }
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
+            for (int i = 0; i < CNT; ++i) {
                 float sm[8];
                 sv[i].to_f32(sm);
-                float xs[RG][8];
 #pragma unroll
                 for (int g = 0; g < RG; ++g) {
-                    xv[i][g].to_f32(xs[g]);
+                    if (16 * g >= n) break;                  // uniform
+                    float xs[8];
+                    xv[i][g].to_f32(xs);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) xs[g][e] = live[g] && in[i] ? xs[g][e] * sm[e] : 0.f;
-                }
-                if constexpr (sizeof(LT) == 2) {
-                    const v4i zero = {0, 0, 0, 0};
-#pragma unroll
-                    for (int g = 0; g < RG; ++g) {
+                    for (int e = 0; e < 8; ++e) xs[e] = in[i] ? xs[e] * sm[e] : 0.f;
+                    if constexpr (sizeof(LT) == 2) {
+                        const v4i zero = {0, 0, 0, 0};
                         v4i hi, lo;
-                        split_bf16x8(xs[g], hi, lo);
+                        split_bf16x8(xs, hi, lo);
 #pragma unroll
                         for (int b = 0; b < RB; ++b) {
                             const v8bf w = __builtin_bit_cast(v8bf, in[i] ? lv[i][b].a : zero);
                             acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, hi), acc[g][b], 0, 0, 0);
                             acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(v8bf, lo), acc[g][b], 0, 0, 0);
                         }
-                    }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        float w[8];
-                        lv[i][b].to_f32(w);
+                        for (int b = 0; b < RB; ++b) {
+                            float w[8];
+                            lv[i][b].to_f32(w);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-#pragma unroll
-                            for (int g = 0; g < RG; ++g)
-                                acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in[i] ? w[e] : 0.f, xs[g][e], acc[g][b], 0, 0, 0);
+                            for (int e = 0; e < 8; ++e)
+                                acc[g][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in[i] ? w[e] : 0.f, xs[e], acc[g][b], 0, 0, 0);
+                        }
                     }
                 }
             }
-        }
+        };
+        int s0 = st0;
+        const int full = min(st1, K >> 5);                   // steps of 32 whole columns
+        for (; s0 + U <= full; s0 += U) run(s0, std::integral_constant<int, U>{}, std::false_type{});
+        for (; s0 < st1; ++s0) run(s0, std::integral_constant<int, 1>{}, std::true_type{});
 #pragma unroll
         for (int g = 0; g < RG; ++g)
 #pragma unroll
             for (int b = 0; b < RB; ++b) red[wave][(g * RB + b) * 64 + lane] = acc[g][b];
         __syncthreads();
-        // item 64 (RB g + b) + lane: columns 4 (lane / 16) .. of slot lane % 16
+        // item 64 (RB g + b) + lane: columns 4 (lane / 16) .. of place 16 g + lane % 16
 #pragma unroll
         for (int it = wave; it < RG * RB; it += kEdWaves) {
-            const int g = it / RB, b = it % RB;
+            const int g = it / RB, b = it % RB, j = 16 * g + (lane & 15);
             v4f v = red[0][it * 64 + lane];
 #pragma unroll
             for (int w = 1; w < kEdWaves; ++w) v = v + red[w][it * 64 + lane];
-            const int64_t slot = gt.first + 16 * g + (lane & 15);
-            bool mine = false;
-#pragma unroll
-            for (int g2 = 0; g2 < RG; ++g2) mine = mine || (g2 == g && live[g2]);
-            if (b >= nb || slot >= gt.end || !mine) continue;
+            if (b >= nb || j >= n) continue;
+            const int64_t slot = gt.first + list[j];
             const int c = c0 + 16 * b + 4 * (lane >> 4);
             *reinterpret_cast<v4f*>(a.u + slot * r + c) = v;
             if (a.u_hl == nullptr) continue;                 // rank <= 64: also as bf16 hi | lo
@@ -557,7 +556,7 @@ __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const
             *reinterpret_cast<v2i*>(p) = v2i{static_cast<int32_t>(h0), static_cast<int32_t>(h1)};
             *reinterpret_cast<v2i*>(p + 128) = v2i{static_cast<int32_t>(l0), static_cast<int32_t>(l1)};
         }
-        __syncthreads();                                     // red is free for the next modality
+        __syncthreads();                                     // red and list are free for the next modality
     }
 }
 
@@ -566,9 +565,10 @@ __global__ __launch_bounds__(64 * kEdWaves, 4) void k_expert_stage1(const XT* __
                                                                  const LT* __restrict__ l_down,
                                                                  ExpertStage1 a, TileExtra ex) {
     __shared__ __attribute__((aligned(16))) v4f red[kEdWaves][RG * RB * 64];
+    __shared__ int list[64];
     const int64_t b = linear_block() - a.downs;
     if (b < 0) {
-        expert_down_tile<XT, LT, RG, RB, U>(x, l_down, a, ex, red);
+        expert_down_tile<XT, LT, RG, RB, U>(x, l_down, a, ex, red, list);
     } else if (a.row_group) {
         if (b < a.T) sq_row<XT, 64 * kEdWaves, 2>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, b, false);
     } else {
@@ -673,8 +673,8 @@ static hipError_t launch_stage1_t(const void* x, const void* l_down, ExpertStage
     } while (0)
     constexpr bool kNarrow = sizeof(XT) == 2 && sizeof(LT) == 2;
     if (most <= 512) MASQ_STAGE1(1, (kNarrow ? 4 : 2));
-    else if (most <= 1024 || RB > 2) MASQ_STAGE1(2, 2);
-    else MASQ_STAGE1((RB > 2 ? 2 : 4), 2);
+    else if (most <= 1024 || RB > 2) MASQ_STAGE1(2, (kNarrow ? 2 : 1));
+    else MASQ_STAGE1((RB > 2 ? 2 : 4), (kNarrow ? 2 : 1));
 #undef MASQ_STAGE1
     return hipGetLastError();
 }
