@@ -91,8 +91,31 @@ __device__ __forceinline__ float logistic(float z) {
 }
 template <bool EXACT>
 __device__ __forceinline__ float act_silu(float z) { return z * logistic<EXACT>(z); }
-// erfc, unlike 1 + erf, keeps its relative accuracy for negative z, where it is small
-__device__ __forceinline__ float act_gelu(float z) { return 0.5f * z * erfcf(z * -0.70710678118654752f); }
+// z Phi(z) = z erfc(-z / sqrt 2) / 2: erfc, unlike 1 + erf, keeps its relative
+// accuracy for negative z, where it is small.  Results that are rounded to bf16
+// take erfc(x) = t 2^(Q(t) - x^2 log2 e), t = 1 / (1 + x / 2), for x >= 0, with the
+// degree-9 Chebyshev interpolant Q of log2(erfc(x) e^(x^2) / t) over x in [0, 10],
+// off by 2.5e-7 of the value in fp32 (a residual may cancel the result, so the
+// output's rounding is no measure of what this may be off by).  The largest
+// listed layer: @@ us where erfcf takes @@.
+template <bool EXACT>
+__device__ __forceinline__ float act_gelu(float z) {
+    if constexpr (EXACT) {
+        return 0.5f * z * erfcf(z * -0.70710678118654752f);
+    } else {
+        constexpr float kQ[10] = {-1.8256655931472778f, 1.4409384727478027f, 0.5558468103408813f,
+                                  0.05972175672650337f, -0.0281441118568182f, -0.057514917105436325f,
+                                  -1.0769284963607788f, 1.724493384361267f, -1.0063326358795166f,
+                                  0.21358530223369598f};
+        const float x = fabsf(z) * 0.70710678118654752f;
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.5f, x, 1.f));
+        float q = kQ[9];
+#pragma unroll
+        for (int i = 8; i >= 0; --i) q = fmaf(q, t, kQ[i]);
+        const float e = t * __builtin_amdgcn_exp2f(fmaf(x * -1.44269504f, x, q));
+        return 0.5f * z * (z > 0.f ? 2.f - e : e);
+    }
+}
 template <bool EXACT>
 __device__ __forceinline__ float act_gelu_tanh(float z) {   // (1 + tanh t) / 2 = 1 / (1 + exp(-2 t))
     return z * logistic<EXACT>(1.5957691216057308f * (z + 0.044715f * (z * z * z)));
@@ -108,7 +131,7 @@ __device__ __forceinline__ void activate(int act, float (&v)[N]) {
             break;
         case kActGelu:
 #pragma unroll
-            for (int e = 0; e < N; e += STEP) v[e] = act_gelu(v[e]);
+            for (int e = 0; e < N; e += STEP) v[e] = act_gelu<kExact>(v[e]);
             break;
         case kActGeluTanh:
 #pragma unroll

@@ -114,20 +114,22 @@ def test_residual_in_place(ops, T, gated):
     assert got.data_ptr() == buf.data_ptr() and torch.equal(got, want)
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
-def test_activations_at_large_arguments(ops, act):
+def test_activations_over_their_range(ops, act, io):
     # codes of +-127 and steps that put z from -1e6 to 1e6, zeros among them
-    K, N, T = 64, 64, 8
-    x = torch.ones((T, K), device="cuda")
+    K, N, T = 64, 4096, 8
+    x = torch.ones((T, K), device="cuda", dtype=DT[io])
     x[3] = 0
     codes = torch.full((N, K), 127, device="cuda", dtype=torch.int8)
     codes[::2] = -127
     scale = (10.0 ** torch.linspace(-9, 3, N, device="cuda")).float()
+    scale[:2048] = torch.linspace(0, 15, 2048, device="cuda") / (127 * 64)
     inv, mod = torch.ones((1, K), device="cuda"), torch.zeros(T, device="cuda", dtype=torch.int32)
     got = ops.Linear(inv, codes, scale).fused(x, mod, act=act)
     z, e = ref.layer(x, mod, inv, codes, scale, None, None)
     assert torch.isfinite(got).all() and (got[3] == 0).all()
-    ref.assert_close(got, *ref.finish(z, e, act, False, None, torch.float32))
+    ref.assert_close(got, *ref.finish(z, e, act, False, None, DT[io]))
 
 
 # ------------------------------------------------------------------ routing
