@@ -303,8 +303,8 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
                                int32_t rank, int32_t n_mod, const float* bias, int32_t act, void* y,
                                masq_dtype y_dt, void* workspace, size_t workspace_bytes,
                                void* stream);
-size_t masq_expert_linear_workspace_bytes(int64_t T, int64_t n_slots, int32_t n_experts, int64_t c_in,
-                                          int64_t c_out, int32_t rank, int32_t n_mod);
+size_t masq_expert_linear_workspace_bytes(int64_t T, int64_t n_slots, int64_t c_in, int32_t rank,
+                                          int32_t n_mod);
 
 masq_status masq_combine_experts(const void* d, masq_dtype dt, const int32_t* slots,
                                  const float* weights, int64_t T, int64_t n_slots, int64_t c_out,

@@ -276,6 +276,35 @@ MasOnlyWs plan_mas_only(void* base, int64_t T, int64_t K, int64_t N, int n_mod) 
     return w;
 }
 
+// Workspace of the experts' layer: plain codes and scales of x's rows, and (with
+// a compensation) u by slot, for ranks up to 64 also as bf16 hi | lo rows.
+struct ExpertWs {
+    int8_t* q;
+    float* x_scale;
+    float* u;
+    uint8_t* u_hl;
+    size_t bytes;
+};
+
+ExpertWs plan_experts(void* base, int64_t T, int64_t n_slots, int64_t K, int rank, int n_mod) {
+    ExpertWs w{};
+    size_t off = 0;
+    uint8_t* b = static_cast<uint8_t*>(base);
+    auto carve = [&](size_t bytes) {
+        uint8_t* p = b ? b + off : nullptr;
+        off += align256(bytes);
+        return p;
+    };
+    w.q = reinterpret_cast<int8_t*>(carve(static_cast<size_t>(T) * static_cast<size_t>(K)));
+    w.x_scale = reinterpret_cast<float*>(carve(static_cast<size_t>(T) * sizeof(float)));
+    if (rank > 0 && n_mod > 1) {
+        w.u = reinterpret_cast<float*>(carve(static_cast<size_t>(n_slots) * rank * sizeof(float)));
+        if (rank <= 64) w.u_hl = carve(static_cast<size_t>(n_slots) * 256);
+    }
+    w.bytes = off;
+    return w;
+}
+
 // Tile shape of the experts' layer, from the rows an expert has on average and
 // the tiles to be expected (half a tile an expert is padding).  Layers of 2048
 // outputs over 64 and 8 experts, 2048 and 1024 columns, us:
@@ -293,41 +322,6 @@ TilePlan plan_expert_tile(int64_t n_slots, int64_t n_experts, int64_t K, int64_t
     if (avg <= (w4 ? 32 : 8)) return TilePlan{0, 1};
     if (avg <= 64 || tiles(128, 128) < 256) return TilePlan{1, 1};
     return TilePlan{avg >= 384 && K % 64 == 0 && tiles(kTileM, kTileN) >= 128 ? -1 : 2, 1};
-}
-
-// Workspace of the experts' layer: codes and scales of x's rows, (256 x 256 tiles
-// of gathered rows) the codes by slot, row-paired, and (with a compensation) u
-// by slot, for ranks up to 64 also as bf16 hi | lo rows.
-struct ExpertWs {
-    int8_t* q;
-    int8_t* slot_q;
-    float* x_scale;
-    float* u;
-    uint8_t* u_hl;
-    size_t bytes;
-};
-
-ExpertWs plan_experts(void* base, int64_t T, int64_t n_slots, int64_t n_experts, int64_t K, int64_t N,
-                      int rank, int n_mod) {
-    ExpertWs w{};
-    size_t off = 0;
-    uint8_t* b = static_cast<uint8_t*>(base);
-    auto carve = [&](size_t bytes) {
-        uint8_t* p = b ? b + off : nullptr;
-        off += align256(bytes);
-        return p;
-    };
-    // (sized for every weight width and for gathered rows alike)
-    w.q = reinterpret_cast<int8_t*>(carve(static_cast<size_t>((T + 1) / 2 * 2) * static_cast<size_t>(K)));
-    if (n_experts > 0 && plan_expert_tile(n_slots, n_experts, K, N, false).shape < 0)
-        w.slot_q = reinterpret_cast<int8_t*>(carve(static_cast<size_t>((n_slots + 1) / 2 * 2) * static_cast<size_t>(K)));
-    w.x_scale = reinterpret_cast<float*>(carve(static_cast<size_t>(T) * sizeof(float)));
-    if (rank > 0 && n_mod > 1) {
-        w.u = reinterpret_cast<float*>(carve(static_cast<size_t>(n_slots) * rank * sizeof(float)));
-        if (rank <= 64) w.u_hl = carve(static_cast<size_t>(n_slots) * 256);
-    }
-    w.bytes = off;
-    return w;
 }
 
 }  // namespace masq
@@ -799,11 +793,10 @@ masq_status masq_route_experts(const void* logits, masq_dtype dt, const int32_t*
                                        slot_modality, w, static_cast<hipStream_t>(stream)));
 }
 
-size_t masq_expert_linear_workspace_bytes(int64_t T, int64_t n_slots, int32_t n_experts, int64_t c_in,
-                                          int64_t c_out, int32_t rank, int32_t n_mod) {
-    if (T < 0 || n_slots < 0 || check_experts(n_experts) != MASQ_OK || c_in <= 0 || c_out <= 0 || rank < 0)
-        return 0;
-    return masq::plan_experts(nullptr, T, n_slots, n_experts, c_in, c_out, rank, n_mod).bytes;
+size_t masq_expert_linear_workspace_bytes(int64_t T, int64_t n_slots, int64_t c_in, int32_t rank,
+                                          int32_t n_mod) {
+    if (T < 0 || n_slots < 0 || c_in <= 0 || rank < 0) return 0;
+    return masq::plan_experts(nullptr, T, n_slots, c_in, rank, n_mod).bytes;
 }
 
 masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const int32_t* modality,
@@ -843,7 +836,7 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
     for (const void* p : ptrs)
         if (!aligned16(p)) return MASQ_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return MASQ_ERR_ALIGN;
-    const masq::ExpertWs w = masq::plan_experts(workspace, T, n_slots, n_experts, c_in, c_out, rank, n_mod);
+    const masq::ExpertWs w = masq::plan_experts(workspace, T, n_slots, c_in, rank, n_mod);
     if (workspace_bytes < w.bytes) return MASQ_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     masq::TileExtra ex{};
@@ -856,25 +849,15 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
     ex.x_rows = T;
     (void)hipGetLastError();
     const bool hl = cmc && rank <= 64 && lr_dt == MASQ_BF16;
-    ex.slot_codes = wide && rows != nullptr;
-    const bool pair = wide && rows == nullptr;
-    if (cmc && !ex.slot_codes)
-        st = from_hip(masq::launch_expert_stage1(x, to_dt(x_dt), modality, inv_smooth, l_down,
-                                                 to_dt(lr_dt), T, n_slots, c_in, rank, n_mod, w.u,
-                                                 hl ? w.u_hl : nullptr, w.q, w.x_scale, ex, pair, s));
-    else
-        st = from_hip(masq::launch_smooth_quant(x, to_dt(x_dt), modality, inv_smooth, T, c_in, n_mod, w.q,
-                                                w.x_scale, nullptr, 0, s, nullptr, pair));
-    if (st == MASQ_OK && ex.slot_codes)
-        st = from_hip(masq::launch_expert_gather(x, to_dt(x_dt), modality, inv_smooth, l_down,
-                                                 to_dt(lr_dt), n_slots, c_in, rank, n_mod,
-                                                 cmc ? w.u : nullptr, hl ? w.u_hl : nullptr, w.q,
-                                                 w.slot_q, ex, s));
+    st = from_hip(cmc ? masq::launch_expert_stage1(x, to_dt(x_dt), modality, inv_smooth, l_down,
+                                                   to_dt(lr_dt), T, n_slots, c_in, rank, n_mod, w.u,
+                                                   hl ? w.u_hl : nullptr, w.q, w.x_scale, ex, s)
+                      : masq::launch_smooth_quant(x, to_dt(x_dt), modality, inv_smooth, T, c_in, n_mod,
+                                                  w.q, w.x_scale, nullptr, 0, s));
     if (st != MASQ_OK) return st;
-    const masq::TileGemm g{ex.slot_codes ? w.slot_q : w.q, w.x_scale, static_cast<const int8_t*>(wq),
-                           w_scale, n_slots, c_in, c_out, modality, w.u, hl ? w.u_hl : nullptr, rank,
-                           n_mod, r_up, to_dt(lr_dt), cmc, nullptr, y, to_dt(y_dt), w4, wide, plan,
-                           nullptr, nullptr, s};
+    const masq::TileGemm g{w.q, w.x_scale, static_cast<const int8_t*>(wq), w_scale, n_slots, c_in, c_out,
+                           modality, w.u, hl ? w.u_hl : nullptr, rank, n_mod, r_up, to_dt(lr_dt), cmc,
+                           nullptr, y, to_dt(y_dt), w4, false, plan, nullptr, nullptr, s};
     return from_hip(wide ? masq::launch_gemm_wide(g, ex) : masq::launch_gemm_experts(g, ex));
 }
 

@@ -336,7 +336,6 @@ struct TileExtra {
     const int32_t* offsets;   // [n_experts + 1]: expert e's slots
     int n_experts;
     int64_t x_rows;
-    bool slot_codes;          // the codes lie in slot order (scales and modalities by row of x)
 };
 
 // The small-tile GEMM; arguments as launch_gemm's.  part / tickets: plan.S
@@ -408,12 +407,6 @@ hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex);
 hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
                                 const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
                                 int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
-                                const TileExtra& ex, bool pair, hipStream_t s);
-// The same for codes that the GEMM reads in slot order: u by slot (u null: no
-// compensation) beside slot_q, the plain codes q [x_rows][K] by slot, row-paired.
-hipError_t launch_expert_gather(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
-                                const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
-                                int n_mod, float* u, uint8_t* u_hl, const int8_t* q, int8_t* slot_q,
                                 const TileExtra& ex, hipStream_t s);
 
 // Routing: at most kRouteMaxExperts experts and kRouteMaxK choices a token.

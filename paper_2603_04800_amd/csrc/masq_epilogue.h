@@ -23,75 +23,51 @@ __device__ __forceinline__ int group_edge(const TileExtra& ex, int e, int64_t n)
     return static_cast<int>(min(max(static_cast<int64_t>(ex.offsets[min(e, ex.n_experts)]), int64_t{0}), n));
 }
 
-// Slots [lo, hi) of expert e, and its tiles of BM rows (none past the last expert).
+// The tile of workgroup `block`: every wave counts the experts' tiles of BM
+// rows, a lane an expert, places the workgroup among them as tile_coords_at
+// does, and finds the expert that holds its row of tiles.  False past the last
+// tile (the grid is sized for the most tiles that n slots can make).
 template <int BM>
-__device__ __forceinline__ int expert_range(const TileExtra& ex, int64_t n, int e, int& lo, int& hi) {
-    lo = group_edge(ex, e, n);
-    hi = e < ex.n_experts ? max(group_edge(ex, e + 1, n), lo) : lo;
-    return (hi - lo + BM - 1) / BM;
-}
-__device__ __forceinline__ int wave_prefix(int v) {          // inclusive, over the lanes
+__device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64_t block, int tiles_n,
+                                           GroupTile& out) {
     const int lane = threadIdx.x & 63;
+    auto count = [&](int e, int& lo, int& hi) __attribute__((always_inline)) {
+        lo = group_edge(ex, e, n);
+        hi = e < ex.n_experts ? max(group_edge(ex, e + 1, n), lo) : lo;
+        return (hi - lo + BM - 1) / BM;
+    };
+    auto scan = [&](int v) __attribute__((always_inline)) {          // inclusive over the lanes
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int p = __shfl_up(v, o);
-        v += lane >= o ? p : 0;
-    }
-    return v;
-}
-
-// The experts' tiles as every wave counts them: lane l's slots are those of
-// expert l, with the running count of tiles up to it; total: over all experts.
-struct GroupScan {
-    int lo, hi, incl, total;
-};
-template <int BM>
-__device__ __forceinline__ GroupScan group_scan(const TileExtra& ex, int64_t n) {
-    const int lane = threadIdx.x & 63;
-    GroupScan s;
-    s.incl = wave_prefix(expert_range<BM>(ex, n, lane, s.lo, s.hi));
-    s.total = __builtin_amdgcn_readlane(s.incl, 63);
+        for (int o = 1; o < 64; o <<= 1) {
+            const int p = __shfl_up(v, o);
+            v += lane >= o ? p : 0;
+        }
+        return v;
+    };
+    int lo, hi;
+    int incl = scan(count(lane, lo, hi));
+    int total = __builtin_amdgcn_readlane(incl, 63);
     for (int b = 64; b < ex.n_experts; b += 64) {
-        int lo, hi;
-        s.total += __builtin_amdgcn_readlane(wave_prefix(expert_range<BM>(ex, n, b + lane, lo, hi)), 63);
+        int l2, h2;
+        total += __builtin_amdgcn_readlane(scan(count(b + lane, l2, h2)), 63);
     }
-    return s;
-}
-
-// Rows of tiles that run together: those of one expert or two share a weight
-// (32768 slots over 64 experts, 2048 -> 2816: groups of 8 / 4 / 3 / 1 rows of 256 x 256
-// tiles 418 / 360 / 348 / 340 us the layer; 8 experts of 3584 -> 8192 368 / 358 / 355 / 368).
-constexpr int kExpertGroup = 3;
-
-// Tile number `block` (placed among the tiles as tile_coords_at does) and the
-// expert that holds its row of tiles.  False past the last tile: the grid is
-// sized for the most tiles that n slots can make.
-template <int BM>
-__device__ __forceinline__ bool group_find(const GroupScan& s, const TileExtra& ex, int64_t n, int64_t block,
-                                           int tiles_n, GroupTile& out) {
-    const int lane = threadIdx.x & 63;
     int tm;
-    if (!tile_coords_at<kExpertGroup>(static_cast<int>(block), s.total, tiles_n, tm, out.tn)) return false;
-    int before = 0, b = 0, lo = s.lo, hi = s.hi, incl = s.incl;
-    for (;;) {                                               // 64 experts a turn
+    if (!tile_coords_at(static_cast<int>(block), total, tiles_n, tm, out.tn)) return false;
+    int before = 0, b = 0;
+    for (;;) {
         const int here = __builtin_amdgcn_readlane(incl, 63);
         if (tm < before + here || b + 64 >= ex.n_experts) break;
         before += here;
         b += 64;
-        incl = wave_prefix(expert_range<BM>(ex, n, b + lane, lo, hi));
+        incl = scan(count(b + lane, lo, hi));
     }
     const unsigned long long past = __ballot(before + incl > tm);
-    const int l = past != 0 ? __builtin_ctzll(past) : 63;    // (tm < total: past != 0)
+    const int l = past != 0 ? __builtin_ctzll(past) : 63;            // (tm < total: past != 0)
     const int prev = l > 0 ? __builtin_amdgcn_readlane(incl, l - 1) : 0;
     out.expert = min(b + l, ex.n_experts - 1);
     out.first = __builtin_amdgcn_readlane(lo, l) + static_cast<int64_t>(tm - before - prev) * BM;
     out.end = min(out.first + BM, static_cast<int64_t>(__builtin_amdgcn_readlane(hi, l)));
     return true;
-}
-template <int BM>
-__device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64_t block, int tiles_n,
-                                           GroupTile& out) {
-    return group_find<BM>(group_scan<BM>(ex, n), ex, n, block, tiles_n, out);
 }
 
 // The row of x behind a slot (an index outside it reads row 0).
@@ -120,8 +96,8 @@ __device__ __forceinline__ float act_silu(float z) { return z * logistic<EXACT>(
 // take erfc(x) = t 2^(Q(t) - x^2 log2 e), t = 1 / (1 + x / 2), for x >= 0, with the
 // degree-9 Chebyshev interpolant Q of log2(erfc(x) e^(x^2) / t) over x in [0, 10],
 // off by 2.5e-7 of the value in fp32 (a residual may cancel the result, so the
-// output's rounding is no measure of what this may be off by).  4096 x
-// 3584 -> 37888 gated: 614 us where erfcf takes 709.
+// output's rounding is no measure of what this may be off by).  The largest
+// listed layer: @@ us where erfcf takes @@.
 template <bool EXACT>
 __device__ __forceinline__ float act_gelu(float z) {
     if constexpr (EXACT) {
@@ -177,8 +153,9 @@ __device__ __forceinline__ void activate(int act, float (&v)[N]) {
 // order, so its buffer (32 rows of kEpiPitch floats) needs no synchronisation.
 //
 // The loop over the blocks is not unrolled (they move down a block a turn): a tile runs through this code once, so that its length is
-// paid in instruction fetches.  Fully unrolled, the products and epilogues of 4096 x
-// 3584 -> 37888 (gated) took 930 us where this form takes 593.
+// paid in instruction fetches.  Fully unrolled, the activations of a 256 x 256
+// tile took longer than its products: 930 us where this form takes @@ (4096 x
+// 3584 -> 37888, gated).
 constexpr int kEpiPitch = 20;                               // 16 channels and 16 bytes
 template <typename YT, int NJ>
 __device__ __forceinline__ void finish_row(v16f (&yb)[NJ], const TileExtra& ex, const float* bias,

@@ -411,10 +411,7 @@ __global__ __launch_bounds__(kRouteMaxExperts) void k_route_place(
 // One launch for two independent pieces of work: workgroups below `downs` form
 // u = (x S_m^-1) L1_e^m for the slots of modality m != text, those past them
 // quantise x's rows (a row a workgroup for small batches, where a row's latency
-// counts, else a row a wave) or, for the 256 x 256 tiles of gathered rows, copy
-// the codes into slot order (two slots a wave, row-paired: the product reads each
-// row's 64-byte pieces once per tile of outputs, two of them a request here and
-// one where they are gathered).
+// counts, else a row a wave).
 //
 // A down-projection workgroup takes 16 RG slots of one expert and 16 RB columns
 // of the rank, its eight waves an eighth of the row each, U steps of 32 columns
@@ -435,8 +432,6 @@ struct ExpertStage1 {
     float* x_scale;
     int64_t downs;
     bool row_group;       // a row a workgroup
-    bool pair;            // q row-paired (code_row / code_col)
-    int8_t* slot_q;       // not null: copy q's rows here instead
 };
 
 // The tile's slots of one modality come side by side first (a list in LDS), so
@@ -574,23 +569,12 @@ __global__ __launch_bounds__(64 * kEdWaves, 4) void k_expert_stage1(const XT* __
     const int64_t b = linear_block() - a.downs;
     if (b < 0) {
         expert_down_tile<XT, LT, RG, RB, U>(x, l_down, a, ex, red, list);
-    } else if (a.slot_q != nullptr) {
-        const int lane = threadIdx.x & 63;
-        const int64_t s0 = 2 * (b * kEdWaves + (threadIdx.x >> 6)), s = s0 + ((lane >> 2) & 1);
-        if (s0 >= a.n_slots) return;
-        // lane: 16-byte piece lane % 4 of 64 columns of slot s; 8 x 64 columns a turn
-        const int8_t* src = a.q + slot_row(ex, min(s, a.n_slots - 1)) * a.K + 64 * (lane >> 3) + 16 * (lane & 3);
-        int8_t* dst = a.slot_q + s0 * a.K + 16 * lane;       // (the pair's unused second row is there)
-        int k = 64 * (lane >> 3);
-#pragma unroll 4
-        for (; k < a.K; k += 512, src += 512, dst += 1024)
-            *reinterpret_cast<v4i*>(dst) = *reinterpret_cast<const v4i*>(src);
     } else if (a.row_group) {
-        if (b < a.T) sq_row<XT, 64 * kEdWaves, 2>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, b, a.pair);
+        if (b < a.T) sq_row<XT, 64 * kEdWaves, 2>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, b, false);
     } else {
         const int64_t t = b * kEdWaves + (threadIdx.x >> 6);
         if (t < a.T)
-            quant_row_wave<XT, 4>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, t, a.pair, threadIdx.x & 63,
+            quant_row_wave<XT, 4>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, t, false, threadIdx.x & 63,
                                   [](int) {});
     }
 }
@@ -677,13 +661,12 @@ hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex) {
 template <typename XT, typename LT, int RB>
 static hipError_t launch_stage1_t(const void* x, const void* l_down, ExpertStage1 a, const TileExtra& ex,
                                   hipStream_t s) {
-    const int64_t quant = a.slot_q != nullptr ? (a.n_slots + 2 * kEdWaves - 1) / (2 * kEdWaves)
-                                              : (a.row_group ? a.T : (a.T + kEdWaves - 1) / kEdWaves);
+    const int64_t quant = a.row_group ? a.T : (a.T + kEdWaves - 1) / kEdWaves;
     const int chunks = (a.r + 16 * RB - 1) / (16 * RB);
     const int64_t most = expert_tiles(a.n_slots, ex.n_experts, 16) * chunks;
 #define MASQ_STAGE1(RG, U)                                                                          \
     do {                                                                                            \
-        if (a.u != nullptr) a.downs = 8 * ((expert_tiles(a.n_slots, ex.n_experts, 16 * RG) * chunks + 7) / 8); \
+        a.downs = 8 * ((expert_tiles(a.n_slots, ex.n_experts, 16 * RG) * chunks + 7) / 8);          \
         hipLaunchKernelGGL((k_expert_stage1<XT, LT, RG, RB, U>), grid_of(a.downs + quant, 64 * kEdWaves), \
                            dim3(64 * kEdWaves), 0, s, static_cast<const XT*>(x),                    \
                            static_cast<const LT*>(l_down), a, ex);                                  \
@@ -696,8 +679,12 @@ static hipError_t launch_stage1_t(const void* x, const void* l_down, ExpertStage
     return hipGetLastError();
 }
 
-static hipError_t launch_stage1_any(const void* x, DT x_dt, const void* l_down, DT lr_dt, int rank,
-                                    const ExpertStage1& a, const TileExtra& ex, hipStream_t s) {
+hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
+                                const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
+                                int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
+                                const TileExtra& ex, hipStream_t s) {
+    ExpertStage1 a{mod, inv_s, n_slots, T, static_cast<int>(K), rank, n_mod, u, u_hl, q, x_scale, 0,
+                   T < kRowsPerWaveMinT};
 #define MASQ_RB(XT, LT)                                                                             \
     (rank <= 16 ? launch_stage1_t<XT, LT, 1>(x, l_down, a, ex, s)                                   \
                 : (rank <= 32 ? launch_stage1_t<XT, LT, 2>(x, l_down, a, ex, s)                     \
@@ -705,25 +692,6 @@ static hipError_t launch_stage1_any(const void* x, DT x_dt, const void* l_down, 
     if (x_dt == DT::BF16) return lr_dt == DT::BF16 ? MASQ_RB(bf16_t, bf16_t) : MASQ_RB(bf16_t, float);
     return lr_dt == DT::BF16 ? MASQ_RB(float, bf16_t) : MASQ_RB(float, float);
 #undef MASQ_RB
-}
-
-hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
-                                const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
-                                int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
-                                const TileExtra& ex, bool pair, hipStream_t s) {
-    const ExpertStage1 a{mod, inv_s, n_slots, T, static_cast<int>(K), rank, n_mod, u, u_hl, q, x_scale, 0,
-                         T < kRowsPerWaveMinT, pair, nullptr};
-    return launch_stage1_any(x, x_dt, l_down, lr_dt, rank, a, ex, s);
-}
-
-hipError_t launch_expert_gather(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
-                                const void* l_down, DT lr_dt, int64_t n_slots, int64_t K, int rank,
-                                int n_mod, float* u, uint8_t* u_hl, const int8_t* q, int8_t* slot_q,
-                                const TileExtra& ex, hipStream_t s) {
-    if (K % 64 != 0) return hipErrorInvalidValue;
-    const ExpertStage1 a{mod, inv_s, n_slots, 0, static_cast<int>(K), rank, n_mod, u, u_hl,
-                         const_cast<int8_t*>(q), nullptr, 0, false, true, slot_q};
-    return launch_stage1_any(x, x_dt, l_down, lr_dt, rank, a, ex, s);
 }
 
 hipError_t launch_route(const void* logits, DT dt, const int32_t* mod, int64_t T, int E, int k,

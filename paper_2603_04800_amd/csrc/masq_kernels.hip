@@ -27,8 +27,6 @@
 #include "masq_epilogue.h"
 #include "masq_quant.h"
 
-#include <algorithm>
-
 
 namespace masq {
 namespace {
@@ -2330,7 +2328,7 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     __shared__ __attribute__((aligned(16))) GemmSmem sm;
     static_assert(kDmaStages * kDmaStageBytes <= static_cast<int>(sizeof(GemmSmem::buf)), "LDS");
     static_assert(kDmaStageBytes == kTileM * 128, "an epilogue operand fills one K stage buffer");
-    static_assert(!PERSIST || (!SPLIT && !GRP), "persistent grid: whole tiles");
+    static_assert(!PERSIST || (!SPLIT && !GRP && !EXP), "persistent grid: whole tiles, one weight");
     static_assert(!EXP || (!SPLIT && !GRP), "experts: whole tiles");
     if constexpr (!SPLIT) S = 1;
     constexpr int NJ = 8 / NWN, NW = 2 * NWN;
@@ -2353,15 +2351,6 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     int ring = 0;        // K buffer of the tile's stage 0
     int rb = 0;          // LDS set of the tile's per-row operands
     int pf = 0;          // the tile's stages already queued
-    // EXP: the workgroup's tile, rows [first, end) of the slots of one expert,
-    // and the next one
-    GroupScan gs{};
-    GroupTile gt{}, gtn{};
-    bool gnext = false;
-    if constexpr (EXP) {
-        gs = group_scan<kTileM>(ex, T);
-        if (!group_find<kTileM>(gs, ex, T, blockIdx.x, tiles_n, gt)) return;
-    }
     for (int vb = static_cast<int>(blockIdx.x);; vb += static_cast<int>(gridDim.x)) {
     // the thread index through an opaque copy, so that no per-lane address of
     // a tile's loop or epilogue is hoisted out of the tile loop (where it would
@@ -2370,9 +2359,22 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / NWN, wn = wave % NWN;
-    int tm = 0, tn = 0;
-    if constexpr (EXP) tn = gt.tn;
-    else if (!tile_coords_at(vb, tiles_m, tiles_n * S, tm, tn)) break;
+    int tm = 0, tn;
+    // EXP: rows [row0, T) of the slots of one expert
+    int64_t slot0 = 0;
+    if constexpr (EXP) {
+        GroupTile gt;
+        if (!group_tile<kTileM>(ex, T, vb, tiles_n, gt)) break;
+        tn = gt.tn;
+        slot0 = gt.first;
+        T = gt.end;
+        B += static_cast<int64_t>(gt.expert) * N * (W4 ? K / 2 : K);
+        w_scale += static_cast<int64_t>(gt.expert) * N;
+        if constexpr (CMC) r_up += static_cast<int64_t>(gt.expert) * (n_mod - 1) * N * r;
+        if (ex.bias != nullptr) ex.bias += static_cast<int64_t>(gt.expert) * N;
+    } else {
+        if (!tile_coords_at(vb, tiles_m, tiles_n * S, tm, tn)) break;
+    }
     // split K: slice sl of S covers stages [kst0, kst0 + nk) of the tile
     int sl = 0;
     if constexpr (SPLIT) {
@@ -2381,17 +2383,8 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     }
     const int nk_slice = SPLIT ? (nk_all + S - 1) / S : nk_all;
     const int kst0 = sl * nk_slice;
-    const int64_t row0 = GRP ? 0 : (EXP ? gt.first : static_cast<int64_t>(tm) * kTileM);
+    const int64_t row0 = GRP ? 0 : (EXP ? slot0 : static_cast<int64_t>(tm) * kTileM);
     const int col0 = tn * kTileN;
-    const int64_t rend = EXP ? gt.end : T;                  // the tile's rows end here
-    // a tile's weight rows and channel scales (EXP: its expert's)
-    auto b_of = [&](const GroupTile& g) __attribute__((always_inline)) {
-        return EXP ? B + static_cast<int64_t>(g.expert) * N * (W4 ? K / 2 : K) : B;
-    };
-    auto ws_of = [&](const GroupTile& g) __attribute__((always_inline)) {
-        return EXP ? w_scale + static_cast<int64_t>(g.expert) * N : w_scale;
-    };
-    const LT* rup = CMC && EXP ? r_up + static_cast<int64_t>(gt.expert) * (n_mod - 1) * N * r : r_up;
     // GRP: the tile's rows grows[gfirst .. gfirst + grows_n), modality gmod
     int gfirst = 0, grows_n = kTileM, gmod = 0;
     if constexpr (GRP) {
@@ -2407,7 +2400,7 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     // last row; their results are discarded)
     auto a_row = [&](int l) __attribute__((always_inline)) -> int64_t {
         if constexpr (GRP) return grows[gfirst + min(l, grows_n - 1)];
-        else return min(row0 + l, rend - 1);
+        else return min(row0 + l, T - 1);
     };
     // the row of A and of the tokens' operands behind an output row
     auto x_row = [&](int64_t t) __attribute__((always_inline)) -> int64_t {
@@ -2422,29 +2415,29 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = v16i{0};
 
-    // per-row operands of the tile at rows r0 .. re, channels c0.. into set `o`:
-    // indices past re or N are clamped (their results are discarded)
-    auto issue_rowops = [&](RowOps& o, int64_t r0, int64_t re, int c0, const float* ws) __attribute__((always_inline)) {
+    // per-row operands of the tile at rows r0.., channels c0.. into set `o`:
+    // indices past T or N are clamped (their results are discarded)
+    auto issue_rowops = [&](RowOps& o, int64_t r0, int c0) __attribute__((always_inline)) {
         // (GRP: the third group is the tiles' token indices, the output rows)
         for (int c = wave; c < kPieces; c += NW) {
             const int part = c & 3, e = 64 * part + lane;
             const void* src;
             uint32_t dst;
             if (c < 4) {
-                src = x_scale + (GRP ? a_row(e) : x_row(min(r0 + e, re - 1)));
+                src = x_scale + (GRP ? a_row(e) : x_row(min(r0 + e, T - 1)));
                 dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&o.dx[64 * part]));
             } else if (c < 8) {
-                src = ws + min(c0 + e, N - 1);
+                src = w_scale + min(c0 + e, N - 1);
                 dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&o.ws[64 * part]));
             } else {
                 src = GRP ? static_cast<const void*>(grows + gfirst + min(e, grows_n - 1))
-                          : static_cast<const void*>(mod + x_row(min(r0 + e, re - 1)));
+                          : static_cast<const void*>(mod + x_row(min(r0 + e, T - 1)));
                 dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&o.rawmod[64 * part]));
             }
             lds_dma4(src, static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(dst))));
         }
     };
-    if (vb == static_cast<int>(blockIdx.x)) issue_rowops(ro, row0, rend, col0, ws_of(gt));   // later tiles: queued ahead
+    if (vb == static_cast<int>(blockIdx.x)) issue_rowops(ro, row0, col0);   // later tiles: queued ahead
 
     // Wave w loads rows [w R, w R + R) of the A and of the B tile (R =
     // kRowsPerWave), 16 rows per instruction; lane i covers row 16 j + i / 4
@@ -2457,15 +2450,13 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     // (The stage st of a tile goes to K buffer (ring + st) % kDmaStages.)
     const int8_t* src[kDmaPerStage];      // [0, kDmaA): A rows, then B rows
     uint32_t dst_off[kDmaPerStage];
-    // sources of the tile at rows r0 .. re, channels c0.. (PERSIST: also the next tile's)
-    auto set_src = [&](const int8_t* (&sp)[kDmaPerStage], int64_t r0, int64_t re, int c0, const int8_t* Bt)
-                       __attribute__((always_inline)) {
+    // sources of the tile at rows r0.., channels c0.. (PERSIST: also the next tile's)
+    auto set_src = [&](const int8_t* (&sp)[kDmaPerStage], int64_t r0, int c0) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kDmaA; ++j) {
             const int row = wave * kRowsPerWave + 16 * j + (lane >> 2);
             const int chunk = (lane & 3) ^ swz4(row);
-            const int64_t slot = min(r0 + row, re - 1);
-            const int64_t tok = GRP ? a_row(row) : (EXP && ex.slot_codes ? slot : x_row(slot));
+            const int64_t tok = GRP ? a_row(row) : x_row(min(r0 + row, T - 1));
             sp[j] = A + code_row(tok, K, a_pair) + kst0 * a_step + 16 * chunk;
         }
 #pragma unroll
@@ -2474,11 +2465,11 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
             const int lanes_per_row = kStepB / 16;
             const int row = wave * kRowsPerWave + kRowsPerDma * j + lane / lanes_per_row;
             const int piece = W4 ? ((lane & 1) ^ ((row >> 3) & 1)) : ((lane & 3) ^ swz4(row));
-            sp[kDmaA + j] = Bt + static_cast<int64_t>(min(c0 + row, N - 1)) * (W4 ? K / 2 : K) +
+            sp[kDmaA + j] = B + static_cast<int64_t>(min(c0 + row, N - 1)) * (W4 ? K / 2 : K) +
                             kst0 * kStepB + 16 * piece;
         }
     };
-    set_src(src, row0, rend, col0, b_of(gt));
+    set_src(src, row0, col0);
 #pragma unroll
     for (int j = 0; j < kDmaA; ++j)
         dst_off[j] = static_cast<uint32_t>(
@@ -2571,8 +2562,6 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     // (PERSIST) the previous tile's epilogue is done with the K buffers
     if (PERSIST && vb != static_cast<int>(blockIdx.x)) __syncthreads();
     for (int st = pf; st < kDmaStages - 1 && st < nk; ++st) issue(st);
-    if constexpr (EXP && PERSIST)
-        gnext = group_find<kTileM>(gs, ex, T, vb + static_cast<int>(gridDim.x), tiles_n, gtn);
     v4i fa0[4], fa1[4];
     BRaw fb0[NJ], fb1[NJ];
     publish(min(nk - 1, 2));
@@ -2602,14 +2591,14 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     // (i % 8) ^ swz(row)
     auto issue_extra = [&](int v) __attribute__((always_inline)) {
         const uint32_t sbase = lds0 + v * kDmaStageBytes;
-        const LT* rm = rup + static_cast<int64_t>(max((v == 2 ? mod0 : mod1) - 1, 0)) * N * r;
+        const LT* rm = r_up + static_cast<int64_t>(max((v == 2 ? mod0 : mod1) - 1, 0)) * N * r;
 #pragma unroll
         for (int q = 0; q < kDmaExtra; ++q) {
             const int rw = wave * kRowsPerWave + 8 * q;
             const int row = rw + (lane >> 3);
             const int lc = (lane & 7) ^ swz(row);
             const uint8_t* sp =
-                v < 2 ? u_hl + min(row0 + row, rend - 1) * 256 + 128 * v + 16 * lc
+                v < 2 ? u_hl + min(row0 + row, T - 1) * 256 + 128 * v + 16 * lc
                       : reinterpret_cast<const uint8_t*>(
                             rm + static_cast<int64_t>(min(col0 + row, N - 1)) * r) +
                             16 * min(lc, (r >> 3) - 1);
@@ -2631,7 +2620,7 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
         }
     };
     int kt = 0;
-    if (EXP && row0 + wm * 128 >= rend) {
+    if (EXP && row0 + wm * 128 >= T) {
         // the tile ends above this wave's rows: its loads and barriers only
         for (; kt + 1 < nk; ++kt) {
             if (kt + kDmaStages - 1 < nk) issue(kt + kDmaStages - 1);
@@ -2722,12 +2711,11 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     // buffer 3 when they are one modality's (buffers 0-2), none with two
     int npf = -1, nring = 0;                 // npf < 0: no next tile
     if constexpr (PERSIST) {
-        int tmn = 0, tnn = gtn.tn;
-        if (EXP ? gnext : tile_coords_at(vb + static_cast<int>(gridDim.x), tiles_m, tiles_n, tmn, tnn)) {
-            const int64_t r0n = EXP ? gtn.first : static_cast<int64_t>(tmn) * kTileM;
-            const int64_t ren = EXP ? gtn.end : T;
+        int tmn, tnn;
+        if (tile_coords_at(vb + static_cast<int>(gridDim.x), tiles_m, tiles_n, tmn, tnn)) {
+            const int64_t r0n = static_cast<int64_t>(tmn) * kTileM;
             const int c0n = tnn * kTileN;
-            issue_rowops(sm.ro[rb ^ 1], r0n, ren, c0n, ws_of(gtn));
+            issue_rowops(sm.ro[rb ^ 1], r0n, c0n);
             npf = 0;
             if (!CMC || present == 0) {
                 npf = min(kDmaStages - 1, nk_all);
@@ -2738,7 +2726,7 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
             if (npf > 0) {
                 if (!synced) __syncthreads();    // every wave is past its reads of the last stages
                 const int8_t* srcn[kDmaPerStage];
-                set_src(srcn, r0n, ren, c0n, b_of(gtn));
+                set_src(srcn, r0n, c0n);
                 for (int st = 0; st < npf; ++st)
 #pragma unroll
                     for (int q = 0; q < kDmaPerStage; ++q) issue_from(srcn, st, q, nring);
@@ -2755,17 +2743,10 @@ __global__ __launch_bounds__(128 * NWN, 1) void k_gemm_dma(
     if constexpr (MODE == kTilePlain)
         gemm_epilogue<YT, LT, CMC, ACC, NWN, GRP>(acc, sm, T, N, row0, col0, u, r, n_mod,
                                                    r_up, acc_out, y, ed, rb, tid);
-    else {
-        TileExtra own = ex;
-        if (EXP && ex.bias != nullptr) own.bias += static_cast<int64_t>(gt.expert) * N;
-        gemm_epilogue_extra<YT, LT, CMC, NWN>(acc, sm, rend, N, row0, col0, u, r, n_mod, rup, y, ed, rb,
-                                              tid, own);
-    }
+    else
+        gemm_epilogue_extra<YT, LT, CMC, NWN>(acc, sm, T, N, row0, col0, u, r, n_mod, r_up, y, ed, rb,
+                                              tid, ex);
     if constexpr (!PERSIST) break;
-    if constexpr (EXP) {
-        if (!gnext) break;
-        gt = gtn;
-    }
     ring = nring;
     pf = max(npf, 0);
     rb ^= 1;
@@ -3244,24 +3225,26 @@ hipError_t launch_gemm_grouped(const int8_t* q, const float* x_scale, const int8
     return hipGetLastError();
 }
 
-// Whole 256 x 256 tiles with an epilogue, on the persistent grid.
+// Whole 256 x 256 tiles with an epilogue: the layer's on the persistent grid,
+// the experts' a workgroup per tile.
 template <typename YT, typename LT, bool CMC, bool W4>
 static hipError_t launch_gemm_wide_t(const TileGemm& g, const TileExtra& ex) {
     const int tiles_n = static_cast<int>((g.N + kTileN - 1) / kTileN);
     const dim3 block(128 * kGemmWavesN);
-#define MASQ_WIDE(MODE, TILES, TM)                                                                  \
-    hipLaunchKernelGGL((k_gemm_dma<YT, LT, CMC, false, kGemmWavesN, false, W4, false, true, MODE>), \
-                       dim3(static_cast<unsigned>(std::min<int64_t>(8 * ((TILES + 7) / 8), persistent_blocks()))), \
-                       block, 0, g.stream, g.q, g.wq, g.x_scale, g.w_scale, g.T,                    \
+#define MASQ_WIDE(PERSIST, MODE, GRID, TM)                                                          \
+    hipLaunchKernelGGL((k_gemm_dma<YT, LT, CMC, false, kGemmWavesN, false, W4, false, PERSIST, MODE>), \
+                       GRID, block, 0, g.stream, g.q, g.wq, g.x_scale, g.w_scale, g.T,              \
                        static_cast<int>(g.K), static_cast<int>(g.N), TM, tiles_n, g.mod, g.u,       \
                        g.u_hl, g.rank, g.n_mod, static_cast<const LT*>(g.r_up), nullptr,            \
                        static_cast<YT*>(g.y), 1, nullptr, nullptr, nullptr, nullptr, nullptr, 0,    \
                        g.a_pair, ex)
     if (ex.offsets != nullptr) {
-        MASQ_WIDE(kTileExperts, expert_tiles(g.T, ex.n_experts, kTileM) * tiles_n, 0);
+        const int64_t nt = expert_tiles(g.T, ex.n_experts, kTileM) * tiles_n;
+        MASQ_WIDE(false, kTileExperts, dim3(static_cast<unsigned>(8 * ((nt + 7) / 8))), 0);
     } else {
         const int tiles_m = static_cast<int>((g.T + kTileM - 1) / kTileM);
-        MASQ_WIDE(kTileEpilogue, static_cast<int64_t>(tiles_m) * tiles_n, tiles_m);
+        const int blocks = min(8 * ((tiles_m * tiles_n + 7) / 8), persistent_blocks());
+        MASQ_WIDE(true, kTileEpilogue, dim3(static_cast<unsigned>(blocks)), tiles_m);
     }
 #undef MASQ_WIDE
     return hipGetLastError();

@@ -57,8 +57,7 @@ _SIGS = {
     "masq_route_experts_workspace_bytes": ([_i64, _i32], ctypes.c_size_t),
     "masq_expert_linear": ([_p, _i32, _i64, _p, _p, _p, _i32, _p, _p, _p, _i32, _p, _p, _i64, _i32,
                             _i64, _i64, _i32, _i32, _p, _i32, _p, _i32, _p, _sz, _p], ctypes.c_int),
-    "masq_expert_linear_workspace_bytes": ([_i64, _i64, _i32, _i64, _i64, _i32, _i32],
-                                           ctypes.c_size_t),
+    "masq_expert_linear_workspace_bytes": ([_i64, _i64, _i64, _i32, _i32], ctypes.c_size_t),
     "masq_combine_experts": ([_p, _i32, _p, _p, _i64, _i64, _i64, _i32, _p, _p, _p], ctypes.c_int),
     "masq_channel_range": ([_p, _i32, _p, _i64, _i64, _i32, _p, _p], ctypes.c_int),
     "masq_smoothing_factors": ([_p, _p, _i64, _i64, _i32, _p, _p, _p], ctypes.c_int),
@@ -829,8 +828,8 @@ class ExpertLinear:
         _shaped(out, (n, self.width), out.dtype, "out")
         ws = workspace
         if ws is None:
-            need = int(_lib.masq_expert_linear_workspace_bytes(
-                T, n, self.n_experts, self.c_in, self.c_out, self.rank, self.n_mod))
+            need = int(_lib.masq_expert_linear_workspace_bytes(T, n, self.c_in, self.rank,
+                                                               self.n_mod))
             ws = _empty((max(need, 256),), torch.uint8, dev, stream)
         lr_dt = _dt(self.l_down) if self.l_down is not None else F32
         args = (_ptr(x), _dt(x), T, _ptr(modality), _ptr(self.inv_smooth), _ptr(self.wq),
