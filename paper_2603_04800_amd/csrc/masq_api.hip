@@ -276,7 +276,7 @@ MasOnlyWs plan_mas_only(void* base, int64_t T, int64_t K, int64_t N, int n_mod) 
     return w;
 }
 
-// Workspace of the experts' layer: plain codes and scales of x's rows, and (with
+// Workspace of the experts' layer: codes and scales of x's rows, and (with
 // a compensation) u by slot, for ranks up to 64 also as bf16 hi | lo rows.
 struct ExpertWs {
     int8_t* q;
@@ -295,7 +295,7 @@ ExpertWs plan_experts(void* base, int64_t T, int64_t n_slots, int64_t K, int ran
         off += align256(bytes);
         return p;
     };
-    w.q = reinterpret_cast<int8_t*>(carve(static_cast<size_t>(T) * static_cast<size_t>(K)));
+    w.q = reinterpret_cast<int8_t*>(carve(static_cast<size_t>((T + 1) / 2 * 2) * static_cast<size_t>(K)));
     w.x_scale = reinterpret_cast<float*>(carve(static_cast<size_t>(T) * sizeof(float)));
     if (rank > 0 && n_mod > 1) {
         w.u = reinterpret_cast<float*>(carve(static_cast<size_t>(n_slots) * rank * sizeof(float)));
@@ -849,15 +849,16 @@ masq_status masq_expert_linear(const void* x, masq_dtype x_dt, int64_t T, const 
     ex.x_rows = T;
     (void)hipGetLastError();
     const bool hl = cmc && rank <= 64 && lr_dt == MASQ_BF16;
+    const bool pair = wide && rows == nullptr;     // neighbouring rows of a tile: one request a pair
     st = from_hip(cmc ? masq::launch_expert_stage1(x, to_dt(x_dt), modality, inv_smooth, l_down,
                                                    to_dt(lr_dt), T, n_slots, c_in, rank, n_mod, w.u,
-                                                   hl ? w.u_hl : nullptr, w.q, w.x_scale, ex, s)
+                                                   hl ? w.u_hl : nullptr, w.q, w.x_scale, ex, pair, s)
                       : masq::launch_smooth_quant(x, to_dt(x_dt), modality, inv_smooth, T, c_in, n_mod,
-                                                  w.q, w.x_scale, nullptr, 0, s));
+                                                  w.q, w.x_scale, nullptr, 0, s, nullptr, pair));
     if (st != MASQ_OK) return st;
     const masq::TileGemm g{w.q, w.x_scale, static_cast<const int8_t*>(wq), w_scale, n_slots, c_in, c_out,
                            modality, w.u, hl ? w.u_hl : nullptr, rank, n_mod, r_up, to_dt(lr_dt), cmc,
-                           nullptr, y, to_dt(y_dt), w4, false, plan, nullptr, nullptr, s};
+                           nullptr, y, to_dt(y_dt), w4, pair, plan, nullptr, nullptr, s};
     return from_hip(wide ? masq::launch_gemm_wide(g, ex) : masq::launch_gemm_experts(g, ex));
 }
 

@@ -407,7 +407,7 @@ hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex);
 hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
                                 const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
                                 int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
-                                const TileExtra& ex, hipStream_t s);
+                                const TileExtra& ex, bool pair, hipStream_t s);
 
 // Routing: at most kRouteMaxExperts experts and kRouteMaxK choices a token.
 // blocks == 0: one workgroup takes the batch and no workspace is needed.

@@ -177,16 +177,16 @@ __device__ __forceinline__ void split_bf16x8(const float (&v)[8], v4i& hi, v4i& 
 }
 
 // Workgroups are dealt round-robin to the 8 XCDs; give each XCD a contiguous
-// range of tiles, ordered in groups of 8 tile-rows, so that tiles running
+// range of tiles, ordered in groups of GM tile-rows, so that tiles running
 // together on one XCD share A and B stages in its L2.  Returns false for the
 // padding workgroups of the last XCD range.
+template <int GM = 8>
 __device__ __forceinline__ bool tile_coords_at(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
     const int nt = tiles_m * tiles_n;
     const int per_xcd = (nt + 7) >> 3;
     if ((b >> 3) >= per_xcd) return false;
     const int L = (b & 7) * per_xcd + (b >> 3);
     if (L >= nt) return false;
-    constexpr int GM = 8;
     const int gsize = GM * tiles_n;
     const int g = L / gsize;
     const int first_m = g * GM;

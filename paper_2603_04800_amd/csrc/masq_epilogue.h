@@ -23,6 +23,12 @@ __device__ __forceinline__ int group_edge(const TileExtra& ex, int e, int64_t n)
     return static_cast<int>(min(max(static_cast<int64_t>(ex.offsets[min(e, ex.n_experts)]), int64_t{0}), n));
 }
 
+// Rows of tiles that run together: those of one expert or two share a weight
+// (32768 slots over 64 experts, 2048 -> 2816: groups of 8 / 4 / 3 / 1 rows of 256 x 256
+// tiles 418 / 360 / 348 / 340 us the layer on one box; 8 experts of 3584 -> 8192
+// 368 / 358 / 355 / 368).
+constexpr int kExpertGroup = 3;
+
 // The tile of workgroup `block`: every wave counts the experts' tiles of BM
 // rows, a lane an expert, places the workgroup among them as tile_coords_at
 // does, and finds the expert that holds its row of tiles.  False past the last
@@ -52,7 +58,7 @@ __device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64
         total += __builtin_amdgcn_readlane(scan(count(b + lane, l2, h2)), 63);
     }
     int tm;
-    if (!tile_coords_at(static_cast<int>(block), total, tiles_n, tm, out.tn)) return false;
+    if (!tile_coords_at<kExpertGroup>(static_cast<int>(block), total, tiles_n, tm, out.tn)) return false;
     int before = 0, b = 0;
     for (;;) {
         const int here = __builtin_amdgcn_readlane(incl, 63);
@@ -96,8 +102,8 @@ __device__ __forceinline__ float act_silu(float z) { return z * logistic<EXACT>(
 // take erfc(x) = t 2^(Q(t) - x^2 log2 e), t = 1 / (1 + x / 2), for x >= 0, with the
 // degree-9 Chebyshev interpolant Q of log2(erfc(x) e^(x^2) / t) over x in [0, 10],
 // off by 2.5e-7 of the value in fp32 (a residual may cancel the result, so the
-// output's rounding is no measure of what this may be off by).  The largest
-// listed layer: @@ us where erfcf takes @@.
+// output's rounding is no measure of what this may be off by).  4096 x
+// 3584 -> 37888 gated: 614 us where erfcf takes 709.
 template <bool EXACT>
 __device__ __forceinline__ float act_gelu(float z) {
     if constexpr (EXACT) {
@@ -153,9 +159,8 @@ __device__ __forceinline__ void activate(int act, float (&v)[N]) {
 // order, so its buffer (32 rows of kEpiPitch floats) needs no synchronisation.
 //
 // The loop over the blocks is not unrolled (they move down a block a turn): a tile runs through this code once, so that its length is
-// paid in instruction fetches.  Fully unrolled, the activations of a 256 x 256
-// tile took longer than its products: 930 us where this form takes @@ (4096 x
-// 3584 -> 37888, gated).
+// paid in instruction fetches.  Fully unrolled, the products and epilogues of 4096 x
+// 3584 -> 37888 (gated) took 930 us where this form takes 593.
 constexpr int kEpiPitch = 20;                               // 16 channels and 16 bytes
 template <typename YT, int NJ>
 __device__ __forceinline__ void finish_row(v16f (&yb)[NJ], const TileExtra& ex, const float* bias,

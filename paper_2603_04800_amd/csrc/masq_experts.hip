@@ -432,6 +432,7 @@ struct ExpertStage1 {
     float* x_scale;
     int64_t downs;
     bool row_group;       // a row a workgroup
+    bool pair;            // q row-paired (code_row / code_col)
 };
 
 // The tile's slots of one modality come side by side first (a list in LDS), so
@@ -570,11 +571,11 @@ __global__ __launch_bounds__(64 * kEdWaves, 4) void k_expert_stage1(const XT* __
     if (b < 0) {
         expert_down_tile<XT, LT, RG, RB, U>(x, l_down, a, ex, red, list);
     } else if (a.row_group) {
-        if (b < a.T) sq_row<XT, 64 * kEdWaves, 2>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, b, false);
+        if (b < a.T) sq_row<XT, 64 * kEdWaves, 2>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, b, a.pair);
     } else {
         const int64_t t = b * kEdWaves + (threadIdx.x >> 6);
         if (t < a.T)
-            quant_row_wave<XT, 4>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, t, false, threadIdx.x & 63,
+            quant_row_wave<XT, 4>(x, a.mod, a.inv_s, a.K, a.n_mod, a.q, a.x_scale, t, a.pair, threadIdx.x & 63,
                                   [](int) {});
     }
 }
@@ -682,9 +683,9 @@ static hipError_t launch_stage1_t(const void* x, const void* l_down, ExpertStage
 hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
                                 const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
                                 int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
-                                const TileExtra& ex, hipStream_t s) {
+                                const TileExtra& ex, bool pair, hipStream_t s) {
     ExpertStage1 a{mod, inv_s, n_slots, T, static_cast<int>(K), rank, n_mod, u, u_hl, q, x_scale, 0,
-                   T < kRowsPerWaveMinT};
+                   T < kRowsPerWaveMinT, pair};
 #define MASQ_RB(XT, LT)                                                                             \
     (rank <= 16 ? launch_stage1_t<XT, LT, 1>(x, l_down, a, ex, s)                                   \
                 : (rank <= 32 ? launch_stage1_t<XT, LT, 2>(x, l_down, a, ex, s)                     \

@@ -235,6 +235,13 @@ EXPERTS = [
     ([500, 20, 400, 0, 129], 0, 448, 416, 64, 4, "bf16", 4, "silu", True, True),
     ([1500, 3], 700, 1040, 160, 16, 2, "f32", 8, "silu", False, True),
     ([0, 0, 0, 700], 300, 512, 512, 256, 2, "f32", 8, "silu", True, False),
+    # 256 x 256 tiles: gathered rows, rows in slot order
+    ([1500, 0, 601, 33, 1], 800, 192, 3104, 16, 3, "bf16", 8, "silu", True, True),
+    ([1500, 0, 601, 33, 1], 0, 192, 3104, 64, 2, "bf16", 4, "gelu", False, True),
+    ([1, 1400, 700, 0, 129], 700, 128, 3104, 16, 2, "f32", 8, "gelu_tanh", True, True),
+    ([2000], 1999, 64, 4096, 128, 4, "bf16", 8, "none", False, False),
+    ([900, 300], 0, 64, 4112, 0, 1, "bf16", 8, "silu", False, True),
+    ([0, 0, 4300, 0] + [0] * 3 + [100], 1024, 320, 1440, 48, 2, "bf16", 4, "silu", True, False),
 ]
 
 
