@@ -321,7 +321,9 @@ TilePlan plan_expert_tile(int64_t n_slots, int64_t n_experts, int64_t K, int64_t
     auto tiles = [&](int64_t bm, int64_t bn) { return (n_slots / bm + (n_experts + 1) / 2) * ((N + bn - 1) / bn); };
     if (avg <= (w4 ? 32 : 8)) return TilePlan{0, 1};
     if (avg <= 64 || tiles(128, 128) < 256) return TilePlan{1, 1};
-    return TilePlan{avg >= 384 && K % 64 == 0 && tiles(kTileM, kTileN) >= 128 ? -1 : 2, 1};
+    // (the grid of 256 x 256 tiles is one launch dimension of 2^32 threads)
+    const int64_t wide = tiles(kTileM, kTileN);
+    return TilePlan{avg >= 384 && K % 64 == 0 && wide >= 128 && wide < (1 << 22) ? -1 : 2, 1};
 }
 
 }  // namespace masq

@@ -40,7 +40,7 @@ __device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64
     auto count = [&](int e, int& lo, int& hi) __attribute__((always_inline)) {
         lo = group_edge(ex, e, n);
         hi = e < ex.n_experts ? max(group_edge(ex, e + 1, n), lo) : lo;
-        return (hi - lo + BM - 1) / BM;
+        return (hi - lo) / BM + ((hi - lo) % BM != 0);
     };
     auto scan = [&](int v) __attribute__((always_inline)) {          // inclusive over the lanes
 #pragma unroll

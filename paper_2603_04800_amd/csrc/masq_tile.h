@@ -384,15 +384,18 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
                                                          acc[0][0][4 * g + 3]};
         }
         __syncthreads();
+        if (wk == 0) {
+#pragma unroll
+            for (int k = 0; k < WK - 1; ++k)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const v4i v = part[k * WN * 256 + 64 * g];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[0][0][4 * g + e] += v[e];
+                }
+        }
+        __syncthreads();                                    // the ring is free for the transposes
         if (wk > 0) return;
-#pragma unroll
-        for (int k = 0; k < WK - 1; ++k)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const v4i v = part[k * WN * 256 + 64 * g];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[0][0][4 * g + e] += v[e];
-            }
     }
     if constexpr (W4) {
 #pragma unroll
@@ -441,7 +444,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
                 for (int e = 0; e < 4; ++e) blk[4 * (c % 4) + e] += v[e];
             }
         }
-    } else {
+    } else if constexpr (WK == 1) {
         __syncthreads();                                    // the ring is free for the transposes
     }
 

@@ -654,7 +654,8 @@ class Linear:
             raise ValueError(f"x must be [T][{self.c_in}]")
         T = x.shape[0]
         shape = (T, self.c_out // 2 if gated else self.c_out)
-        dev = _device_of(x=x, modality=modality, wq=self.wq, inv_smooth=self.inv_smooth, bias=bias,
+        dev = _device_of(x=x, modality=modality, wq=self.wq, inv_smooth=self.inv_smooth,
+                         w_scale=self.w_scale, l_down=self.l_down, r_up=self.r_up, bias=bias,
                          residual=residual, out=out, workspace=workspace)
         _shaped(modality, (T,), torch.int32, "modality")
         _shaped(bias, (self.c_out,), torch.float32, "bias")
@@ -819,7 +820,8 @@ class ExpertLinear:
         T = x.shape[0]
         n = T if rows is None else rows.numel()
         dev = _device_of(x=x, modality=modality, offsets=offsets, rows=rows, wq=self.wq,
-                         inv_smooth=self.inv_smooth, out=out, workspace=workspace)
+                         inv_smooth=self.inv_smooth, w_scale=self.w_scale, l_down=self.l_down,
+                         r_up=self.r_up, bias=self.bias, out=out, workspace=workspace)
         _shaped(modality, (T,), torch.int32, "modality")
         _shaped(offsets, (self.n_experts + 1,), torch.int32, "offsets")
         _shaped(rows, (n,), torch.int32, "rows")

@@ -66,6 +66,7 @@ LAYERS = [
     (1, 64, 32, 0, 1, "bf16", 8, "none", False, True, False),
     (1, 3584, 4608, 64, 2, "bf16", 8, "none", False, True, True),
     (3, 128, 96, 16, 2, "f32", 8, "silu", True, True, True),
+    (5, 80, 48, 16, 2, "bf16", 8, "gelu", False, True, True),          # a small batch with K % 64 != 0
     (16, 8192, 224, 32, 3, "bf16", 8, "gelu", False, True, True),      # decode GEMM, split rows
     (16, 512, 18944, 16, 2, "bf16", 4, "silu", True, False, True),
     (15, 4096, 64, 64, 4, "f32", 4, "gelu_tanh", True, True, False),
@@ -447,6 +448,40 @@ def test_calls_on_two_streams_at_once(ops):
     torch.cuda.synchronize()
     for i, y in enumerate(got):
         assert torch.equal(y, want[i % 2])
+
+
+# ------------------------------------------------------------------ past 2^31 elements
+def test_rows_past_2_31_elements(ops):
+    T, K, N = 70000, 64, 32768
+    c = Case(5, T, K, N, bias=True, residual=True, width=N)
+    lin = ops.Linear(c.inv, c.wq, c.scale)
+    y = lin.fused(c.x, c.mod, bias=c.bias, act="silu", residual=c.res)
+    at = slice(T - 40, T)
+    part = lin.fused(c.x[at].contiguous(), c.mod[at], bias=c.bias, act="silu", residual=c.res[at].contiguous())
+    assert torch.equal(y[at], part)
+    # the same rows as two experts' (the last slots are the second one's)
+    two = ops.ExpertLinear(c.inv, c.wq[None].expand(2, -1, -1).contiguous(), c.scale[None].repeat(2, 1),
+                           bias=c.bias[None].repeat(2, 1), act="silu")
+    z = two(c.x, c.mod, _offsets([T - 100, 100]), out=y)
+    assert torch.equal(z[at], lin.fused(c.x[at].contiguous(), c.mod[at], bias=c.bias, act="silu"))
+    # and combined: token t takes row T - 1 - t
+    slots = torch.arange(T - 1, -1, -1, device="cuda", dtype=torch.int32)[:, None].contiguous()
+    w = torch.ones((T, 1), device="cuda")
+    s = ops.combine_experts(z, slots, w, out=c.res)
+    assert torch.equal(s[:40].flip(0), z[at]) and torch.equal(s[T - 40:].flip(0), z[:40])
+
+
+def test_weights_past_2_31_bytes(ops):
+    E, N, K = 34, 8192, 8192
+    g = _gen(2)
+    wq = torch.zeros((E, N, K), dtype=torch.int8, device="cuda")
+    wq[-1] = torch.randint(-127, 128, (N, K), generator=g, device="cuda").to(torch.int8)
+    scale = torch.full((E, N), 1e-4, device="cuda")
+    x = _randn(g, 9, K).to(torch.bfloat16)
+    mod, inv = torch.zeros(9, dtype=torch.int32, device="cuda"), torch.ones((1, K), device="cuda")
+    got = ops.ExpertLinear(inv, wq, scale)(x, mod, _offsets([0] * (E - 2) + [2, 7]))
+    want = ops.Linear(inv, wq[-1], scale[-1])(x, mod)
+    assert torch.equal(got[2:], want[2:]) and not got[:2].any()
 
 
 def test_results_do_not_vary(ops):
