@@ -149,6 +149,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
     constexpr bool GRP = MODE == kTileExperts;
     constexpr int NW = WM * WN * WK, NT = 64 * NW;
     constexpr int MI = BM / WM / 32, NJ = BN / WN / 32;     // 32 x 32 blocks of a wave
+    constexpr bool kAhead = GRP && MI == 1 && NJ == 1;
     constexpr int kRowB = W4 ? kTsK / 2 : kTsK;             // B bytes per row and stage
     constexpr int kStage = ts_stage_bytes(BM, BN, W4);
     constexpr int kDmaA = BM * kTsK / 1024 / NW, kDmaB = BN * kRowB / 1024 / NW;
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // (WK: waves that share a block take WK-ths of a stage's columns each)
     const int wm = wave / WN % WM, wn = wave % WN, wk = wave / (WM * WN);
-    static_assert(WK == 1 || (GRP && WM == 1 && 4 % WK == 0), "shared blocks: the experts' small tiles");
+    static_assert(WK == 1 || (kAhead && WM == 1 && 4 % WK == 0), "shared blocks: the experts' small tiles");
     int tm, tn;
     // output rows [row0, rend) of the tile; GRP: slots of expert `expert`
     int64_t row0, rend = T;
@@ -270,9 +271,12 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
         const uint8_t* sb = sa + BM * kTsK;
         const int h = lane >> 5;
         const v4i zero = {0, 0, 0, 0};
-        if constexpr (GRP) {
+        if constexpr (kAhead) {
             // every fragment of the stage is read before `between` (the next
-            // stage's DMA), whose issue hides the reads' latency
+            // stage's DMA), whose issue hides the reads' latency (experts' tiles of
+            // one block a wave; with four blocks a wave the 64 registers of a
+            // stage's fragments cost more: 92 -> 98 us at 1024 x 8 rows of 64
+            // experts, 2048 -> 2048)
             constexpr int kN = 4 / WK;
             v4i ga[kN][MI];
             std::conditional_t<W4, v2i, v4i> gb[kN][NJ];
@@ -354,12 +358,12 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
     for (; st + NST - 1 < ns; ++st) {
         publish(NST - 2);
         auto refill = [&]() __attribute__((always_inline)) { issue(st + NST - 1, nxt); };
-        if constexpr (GRP) {
+        if constexpr (kAhead) {
             if (idle) refill();
             else compute(cur, 8, refill);
         } else {
             refill();
-            compute(cur, 8, [] {});
+            if (!idle) compute(cur, 8, [] {});
         }
         cur = cur + 1 == NST ? 0 : cur + 1;
         nxt = nxt + 1 == NST ? 0 : nxt + 1;
