@@ -435,10 +435,27 @@ struct ExpertStage1 {
     bool pair;            // q row-paired (code_row / code_col)
 };
 
+// A fragment's 16 rows lie a row apart in memory, so a load in the MFMA's own
+// order (lane l: row l % 16, columns 8 (l / 16) ..) asks for 64 pieces of 16
+// bytes, one after the other.  The loads go by lane l: row l / 4, columns
+// 8 (l % 4) .. instead, 64 contiguous bytes for four lanes, and the lanes trade
+// their pieces through the LDS crossbar (32768 slots, half of them text, 2048
+// columns, rank 32: 44 -> 40 us).
+//
 // The tile's slots of one modality come side by side first (a list in LDS), so
 // that a group of 16 MFMA columns holds slots that count: a tile of which half
 // is text costs half the loads and products.  A column's sums depend on its own
 // row only, so the columns past the last slot may hold anything.
+__device__ __forceinline__ v4i to_fragment(v4i v, int from) {
+    return v4i{__builtin_amdgcn_ds_bpermute(from, v.x), __builtin_amdgcn_ds_bpermute(from, v.y),
+               __builtin_amdgcn_ds_bpermute(from, v.z), __builtin_amdgcn_ds_bpermute(from, v.w)};
+}
+__device__ __forceinline__ void to_fragment(Raw8<bf16_t>& v, int from) { v.a = to_fragment(v.a, from); }
+__device__ __forceinline__ void to_fragment(Raw8<float>& v, int from) {
+    v.a = __builtin_bit_cast(v4f, to_fragment(__builtin_bit_cast(v4i, v.a), from));
+    v.b = __builtin_bit_cast(v4f, to_fragment(__builtin_bit_cast(v4i, v.b), from));
+}
+
 template <typename XT, typename LT, int RG, int RB, int U>
 __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const LT* __restrict__ l_down,
                                                  const ExpertStage1& a, const TileExtra& ex,
@@ -453,6 +470,7 @@ __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const
     const int nb = min(RB, (r - c0) >> 4);                   // 16-column blocks of the rank
     const int steps = (K + 31) >> 5, per = (steps + kEdWaves - 1) / kEdWaves;
     const int st0 = wave * per, st1 = min(steps, st0 + per);
+    const int from = 4 * (4 * (lane & 15) + (lane >> 4));    // whose piece is this lane's (byte index)
     const int count = static_cast<int>(gt.end - gt.first);
     // lane l: slot l of the tile
     const int row_l = static_cast<int>(slot_row(ex, min(gt.first + lane, gt.end - 1)));
@@ -468,7 +486,7 @@ __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const
         const XT* xp[RG];
 #pragma unroll
         for (int g = 0; g < RG; ++g)                         // (places past n repeat the last slot)
-            xp[g] = x + static_cast<int64_t>(__shfl(row_l, list[min(16 * g + (lane & 15), n - 1)])) * K;
+            xp[g] = x + static_cast<int64_t>(__shfl(row_l, list[min(16 * g + (lane >> 2), n - 1)])) * K;
         v4f acc[RG][RB];
 #pragma unroll
         for (int g = 0; g < RG; ++g)
@@ -484,13 +502,13 @@ __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const
             bool in[CNT];
 #pragma unroll
             for (int i = 0; i < CNT; ++i) {
-                const int k = 32 * (s0 + i) + 8 * (lane >> 4);
-                in[i] = !TAIL || k < K;                      // K % 16 == 0: 8 columns in or out together
-                const int kc = TAIL ? min(k, K - 8) : k;
+                const int kf = 32 * (s0 + i) + 8 * (lane >> 4), kl = 32 * (s0 + i) + 8 * (lane & 3);
+                in[i] = !TAIL || kf < K;                     // K % 16 == 0: 8 columns in or out together
+                const int kc = TAIL ? min(kl, K - 8) : kl;
 #pragma unroll
                 for (int b = 0; b < RB; ++b)
-                    lv[i][b].load(lm + static_cast<int64_t>(c0 + 16 * min(b, nb - 1) + (lane & 15)) * K + kc);
-                sv[i].load(im + kc);
+                    lv[i][b].load(lm + static_cast<int64_t>(c0 + 16 * min(b, nb - 1) + (lane >> 2)) * K + kc);
+                sv[i].load(im + (TAIL ? min(kf, K - 8) : kf));
 #pragma unroll
                 for (int g = 0; g < RG; ++g)
                     if (16 * g < n) xv[i][g].load(xp[g] + kc);               // uniform
@@ -500,9 +518,12 @@ __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const
                 float sm[8];
                 sv[i].to_f32(sm);
 #pragma unroll
+                for (int b = 0; b < RB; ++b) to_fragment(lv[i][b], from);
+#pragma unroll
                 for (int g = 0; g < RG; ++g) {
                     if (16 * g >= n) break;                  // uniform
                     float xs[8];
+                    to_fragment(xv[i][g], from);
                     xv[i][g].to_f32(xs);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) xs[e] = in[i] ? xs[e] * sm[e] : 0.f;
