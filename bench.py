@@ -42,8 +42,8 @@ if ROOT not in sys.path:
 
 INT8_PEAK_TOPS = 5000.0      # MI355X dense int8 MFMA
 HBM_PEAK_GBS = 8000.0        # MI355X HBM3E
-KERNEL_SOURCES = ("paper_2603_04800_amd/csrc/masq_kernels.hip",
-                  "paper_2603_04800_amd/csrc/masq_tile.hip")
+KERNEL_SOURCES = tuple("paper_2603_04800_amd/csrc/" + f for f in (
+    "masq_kernels.hip", "masq_tile.hip", "masq_tile.h", "masq_epilogue.h", "masq_quant.h"))
 
 
 def log(msg):

@@ -25,7 +25,7 @@ __device__ __forceinline__ int group_edge(const TileExtra& ex, int e, int64_t n)
 
 // Rows of tiles that run together: those of one expert or two share a weight
 // (32768 slots over 64 experts, 2048 -> 2816: groups of 8 / 4 / 3 / 1 rows of 256 x 256
-// tiles 418 / 360 / 348 / 340 us the layer on one box; 8 experts of 3584 -> 8192
+// tiles 418 / 360 / 348 / 340 us the layer, on a persistent grid; 8 experts of 3584 -> 8192
 // 368 / 358 / 355 / 368).
 constexpr int kExpertGroup = 3;
 

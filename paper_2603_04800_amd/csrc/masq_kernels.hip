@@ -15,7 +15,7 @@
 //                    dequantisation, then on tiles that hold non-text rows the
 //                    rank-r up-projection u L2^m on bf16 (fp32) MFMA
 //                    accumulating into the dequantised fp32 tile, then the cast
-//                    and store.  (Small tiles: k_gemm_tile in masq_tile.hip.)
+//                    and store.  (Small tiles: k_gemm_tile in masq_tile.h.)
 //   k_lowrank_comp   standalone y += (x S_m^-1 L1^m) L2^m.
 //
 // Bit-exact contract: the smoothing is a single fp32 multiply, the scale and
@@ -2306,6 +2306,20 @@ __device__ __forceinline__ int swz4(int row) { return (row >> 2) & 3; }
 // w_scale + modality N).  A rows and their scales are gathered by the DMA,
 // outputs are written to the tokens' own rows; table entries past *gtab_n
 // (the grid is sized for the largest possible table) exit at once.
+//
+// EXP (the experts' layer): the tile's rows are slots of one expert
+// (group_tile), its weight, scales, factors and bias that expert's; A rows,
+// scales and modalities are gathered by row of x, u and outputs are by slot.
+// A tile that ends above the lower half's rows leaves the four waves of that
+// half their loads and barriers only.  One workgroup a tile, dealt out by the
+// hardware: the persistent grid's fixed shares took 335 us where this takes 316
+// (tiles of unlike cost: 1738 of them, a fifth half empty).  32768 slots of 2048 ->
+// 2816 over 64 experts, gated, rank 32: 290-325 us, 1.2-1.3 P int8 operations
+// a second on the rows that count; the same rows of one layer take 237 us (no
+// padding, a weight that stays in L2), and padding alone makes that 290.
+//
+// MODE kTileEpilogue or kTileExperts: bias, activation and residual past the
+// layer's result (gemm_epilogue_extra).
 //
 // PERSIST (whole tiles of one weight, no split): a grid of at most one
 // workgroup per compute unit walks the tiles blockIdx.x, + gridDim.x, ...
