@@ -79,6 +79,19 @@ TilePlan plan_tile(int64_t T, int64_t K, int64_t N, bool split, bool w4, bool sl
     return p;
 }
 
+// The same for the layer with an epilogue, whose 32 x 64 tiles have two waves a
+// block: batches of 33 to 128 tokens whose 32 x 64 tiles are at most one a compute
+// unit take them, split up to two a unit (us, 64 x 64 tiles / these: 64 tokens,
+// packed 18944 -> 3584 33.9 / 30.3, 3584 -> 3584 19.2 / 17.6; 100 tokens, packed
+// 8192 -> 2048 17.8 / 16.1; 48 of 1024 -> 2048 10.0 / 9.4; past one a unit, 64 of
+// 3584 -> 18944, 26.7 / 28.0).
+TilePlan plan_epilogue_tile(int64_t T, int64_t K, int64_t N, bool w4, bool slow_comp) {
+    const int64_t n = ((T + 31) / 32) * ((N + 63) / 64);
+    if (T <= 32 || T > 128 || n > 256) return plan_tile(T, K, N, true, w4, slow_comp);
+    const int64_t stages = (K + kTileStageK - 1) / kTileStageK;
+    return TilePlan{0, tile_slices(K, static_cast<int>(std::min<int64_t>({512 / n, stages / 10, 8})))};
+}
+
 static size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 
 // Number of k slices of the down-projection.  Small batches (at most 16 row
@@ -195,10 +208,12 @@ static Workspace carve_workspace(void* base, int64_t T, int64_t K, int64_t N, in
 // slices of k_down_lds (down_lds_quarters) are taken where it has room for
 // their partials.
 Workspace plan_workspace(void* base, int64_t T, int64_t K, int64_t N, int rank, int n_mod,
-                         bool w4, bool slow_comp) {
+                         bool w4, bool slow_comp, bool epilogue) {
     const int long_q = 4 * down_lds_chunks(T, K), dl_q = down_lds_quarters(T, K);
     Workspace w = carve_workspace(base, T, K, N, rank, n_mod, TilePlan{-1, 1}, long_q);
-    TilePlan tile = small_path(T, K) ? TilePlan{-1, 1} : plan_tile(T, K, N, true, w4, slow_comp);
+    TilePlan tile = small_path(T, K) ? TilePlan{-1, 1}
+                                     : (epilogue ? plan_epilogue_tile(T, K, N, w4, slow_comp)
+                                                 : plan_tile(T, K, N, true, w4, slow_comp));
     const size_t bytes = w.bytes;
     for (; tile.shape >= 0; tile.S = tile_slices(K, tile.S - 1)) {
         w = carve_workspace(base, T, K, N, rank, n_mod, tile, long_q);
@@ -410,7 +425,7 @@ masq_status fused_stage(const Fused& a, int stage) {
     const bool cmc = a.rank > 0 && a.n_mod > 1;
     const masq::Workspace w =
         masq::plan_workspace(a.workspace, a.T, a.c_in, a.c_out, a.rank, a.n_mod, a.w4,
-                             cmc && (a.lr_dt == MASQ_F32 || a.rank > 64));
+                             cmc && (a.lr_dt == MASQ_F32 || a.rank > 64), a.ex != nullptr);
     hipStream_t s = static_cast<hipStream_t>(a.stream);
     (void)hipGetLastError();
     if ((stage & 1) && masq::small_path(a.T, a.c_in)) {

@@ -181,7 +181,7 @@ struct Workspace {
 };
 
 Workspace plan_workspace(void* base, int64_t T, int64_t K, int64_t N, int rank, int n_mod,
-                         bool w4 = false, bool slow_comp = false);
+                         bool w4 = false, bool slow_comp = false, bool epilogue = false);
 
 // zero_ints / n_zero: optional array the kernel clears on the way (the
 // down-projection's tickets, which must start at zero).

@@ -31,16 +31,16 @@ hipError_t launch_tile_mode(const TileGemm& g, const TileExtra& ex, int tiles_m)
 #define MASQ_TILE(BM, BN, WM, WN, NST, WPE) MASQ_TILE_WK(BM, BN, WM, WN, NST, WPE, 1)
     switch (g.plan.shape) {
         case 0:
+            // two waves a block, each half of a stage's columns
             if constexpr (MODE == kTileExperts) {
-                // two waves a block, each half of a stage's columns; past 16
-                // stages a ring of four (us with one wave and three buffers / two
+                // past 16 stages a ring of four (us with one wave and three buffers / two
                 // and three / two and four: 16 tokens x 8 of 64 experts of 1024
                 // -> 2048 32.1 / 30.9 / 32.6, of 4096 -> 2048 130.3 / 124.0 / 110.9; one
                 // token 19.0 / 18.4 / 18.4)
                 if (g.K > 16 * kTileStageK) MASQ_TILE_WK(32, 64, 1, 2, 4, 2, 2);
                 else MASQ_TILE_WK(32, 64, 1, 2, 3, 2, 2);
             } else {
-                MASQ_TILE(32, 64, 1, 2, 3, 2);
+                MASQ_TILE_WK(32, 64, 1, 2, 4, 2, 2);
             }
             break;
         case 1: MASQ_TILE(64, 64, 2, 2, 3, 3); break;

@@ -147,9 +147,9 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
     int r, int n_mod, const LT* __restrict__ r_up, int32_t* __restrict__ acc_out,
     YT* __restrict__ y, int S, int32_t* __restrict__ part, int* __restrict__ tickets, bool a_pair, TileExtra ex) {
     constexpr bool GRP = MODE == kTileExperts;
-    constexpr int NW = WM * WN * WK, NT = 64 * NW;
+    constexpr int NW = WM * WN * WK;
     constexpr int MI = BM / WM / 32, NJ = BN / WN / 32;     // 32 x 32 blocks of a wave
-    constexpr bool kAhead = GRP && MI == 1 && NJ == 1;
+    constexpr bool kAhead = MODE != kTilePlain && MI == 1 && NJ == 1;
     constexpr int kRowB = W4 ? kTsK / 2 : kTsK;             // B bytes per row and stage
     constexpr int kStage = ts_stage_bytes(BM, BN, W4);
     constexpr int kDmaA = BM * kTsK / 1024 / NW, kDmaB = BN * kRowB / 1024 / NW;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // (WK: waves that share a block take WK-ths of a stage's columns each)
     const int wm = wave / WN % WM, wn = wave % WN, wk = wave / (WM * WN);
-    static_assert(WK == 1 || (kAhead && WM == 1 && 4 % WK == 0), "shared blocks: the experts' small tiles");
+    static_assert(WK == 1 || (kAhead && WM == 1 && 4 % WK == 0), "shared blocks: the small tiles with an epilogue");
     int tm, tn;
     // output rows [row0, rend) of the tile; GRP: slots of expert `expert`
     int64_t row0, rend = T;
@@ -273,8 +273,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
         const v4i zero = {0, 0, 0, 0};
         if constexpr (kAhead) {
             // every fragment of the stage is read before `between` (the next
-            // stage's DMA), whose issue hides the reads' latency (experts' tiles of
-            // one block a wave; with four blocks a wave the 64 registers of a
+            // stage's DMA), whose issue hides the reads' latency (tiles of one block
+            // a wave; with four blocks a wave the 64 registers of a
             // stage's fragments cost more: 92 -> 98 us at 1024 x 8 rows of 64
             // experts, 2048 -> 2048)
             constexpr int kN = 4 / WK;
@@ -399,8 +399,10 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
                 }
         }
         __syncthreads();                                    // the ring is free for the transposes
-        if (wk > 0) return;
+        if (wk > 0 && S == 1) return;
     }
+    const bool owner = WK == 1 || wk == 0;                  // the wave holds sums
+    constexpr int kOwners = 64 * WM * WN;
     if constexpr (W4) {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
@@ -422,12 +424,14 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
         const int tile = tm * tiles_n + tn;
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
             part + static_cast<int64_t>(tile) * S * (BM * BN), 0, S * kSlot, 0x00020000);
+        if (owner) {
 #pragma unroll
-        for (int c = 0; c < kV4; ++c) {
-            const v16i& blk = acc[c / (4 * NJ)][(c / 4) % NJ];
-            const v4i v = {blk[4 * (c % 4)], blk[4 * (c % 4) + 1], blk[4 * (c % 4) + 2],
-                           blk[4 * (c % 4) + 3]};
-            __builtin_amdgcn_raw_buffer_store_b128(v, rs, sl * kSlot + (c * NT + tid) * 16, 0, kPolicy);
+            for (int c = 0; c < kV4; ++c) {
+                const v16i& blk = acc[c / (4 * NJ)][(c / 4) % NJ];
+                const v4i v = {blk[4 * (c % 4)], blk[4 * (c % 4) + 1], blk[4 * (c % 4) + 2],
+                               blk[4 * (c % 4) + 3]};
+                __builtin_amdgcn_raw_buffer_store_b128(v, rs, sl * kSlot + (c * kOwners + tid) * 16, 0, kPolicy);
+            }
         }
         MASQ_WAIT_VMCNT_LGKM0(0);
         __syncthreads();
@@ -437,12 +441,13 @@ __global__ __launch_bounds__(64 * WM * WN * WK, WPE) void k_gemm_tile(
         __syncthreads();
         if (!s_last) return;
         if (tid == 0) __hip_atomic_store(&tickets[tile], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (!owner) return;                                 // (no barrier follows)
         for (int s2 = 0; s2 < S; ++s2) {
             if (s2 == sl) continue;
 #pragma unroll
             for (int c = 0; c < kV4; ++c) {
                 const v4i v = __builtin_amdgcn_raw_buffer_load_b128(
-                    rs, s2 * kSlot + (c * NT + tid) * 16, 0, kPolicy);
+                    rs, s2 * kSlot + (c * kOwners + tid) * 16, 0, kPolicy);
                 v16i& blk = acc[c / (4 * NJ)][(c / 4) % NJ];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) blk[4 * (c % 4) + e] += v[e];

@@ -74,6 +74,8 @@ LAYERS = [
     (32, 4096, 96, 16, 2, "f32", 8, "gelu", True, True, True),         # split into slices
     (33, 1040, 2000, 16, 2, "f32", 8, "gelu", False, True, True),
     (70, 512, 992, 32, 3, "bf16", 8, "silu", True, True, True),
+    (100, 8192, 2048, 16, 2, "bf16", 4, "gelu", True, False, True),    # 32 x 64 tiles in slices
+    (48, 6160, 528, 32, 3, "f32", 8, "silu", False, True, True),
     (64, 18944, 512, 64, 2, "bf16", 4, "none", False, False, True),
     (333, 1040, 720, 128, 2, "bf16", 8, "gelu_tanh", False, True, True),
     (300, 768, 13248, 16, 2, "f32", 8, "silu", True, True, False),     # 128 x 128 tiles
@@ -95,7 +97,8 @@ def test_layer_epilogue(ops, T, K, N, rank, mods, io, bits, act, gated, bias, re
     ref.assert_close(got, *ref.finish(z, e, act, gated, c.res, DT[io]))
 
 
-@pytest.mark.parametrize("T,K,N", [(1, 512, 256), (16, 2048, 512), (40, 512, 512), (400, 1024, 4096)])
+@pytest.mark.parametrize("T,K,N", [(1, 512, 256), (16, 2048, 512), (40, 512, 512), (400, 1024, 4096),
+                                   (50, 8192, 528), (128, 18944, 512), (2304, 320, 6176)])
 def test_epilogue_of_nothing_is_the_layer(ops, T, K, N):
     c = Case(T, T, K, N, rank=16, mods=2)
     c.mod.zero_()
