@@ -118,6 +118,22 @@ def test_residual_in_place(ops, T, gated):
     assert got.data_ptr() == buf.data_ptr() and torch.equal(got, want)
 
 
+@pytest.mark.parametrize("T,K,N", [(7, 256, 96), (60, 512, 512), (400, 320, 4096), (2500, 192, 8480)])
+@pytest.mark.parametrize("xt,yt,lr", [("bf16", "f32", "bf16"), ("f32", "bf16", "f32"), ("bf16", "bf16", "f32")])
+def test_mixed_types(ops, T, K, N, xt, yt, lr):
+    c = Case(T, T, K, N, rank=32, mods=3, io=xt, lr=lr, bias=True)
+    c.mod[::5] = 9                                          # no modality: text
+    c.mod[1::7] = -1
+    res = _randn(_gen(1), T, N // 2).to(DT[yt])
+    lin = ops.Linear(c.inv, c.wq, c.scale, c.ld, c.ru)
+    ws = torch.full((ops.workspace_bytes(T, K, N, 32, 3),), 255, dtype=torch.uint8, device="cuda")   # dirty
+    out = torch.empty((T, N // 2), dtype=DT[yt], device="cuda")
+    got = lin.fused(c.x, c.mod, bias=c.bias, act="gelu_tanh", gated=True, residual=res, out=out, workspace=ws)
+    mod = torch.where((c.mod < 0) | (c.mod > 2), torch.zeros_like(c.mod), c.mod)
+    z, e = ref.layer(c.x, mod, c.inv, c.codes, c.scale, c.ld, c.ru, c.bias)
+    ref.assert_close(got, *ref.finish(z, e, "gelu_tanh", True, res, DT[yt]))
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 def test_activations_over_their_range(ops, act, io):
@@ -277,6 +293,41 @@ def test_experts_leave_rows_past_the_last_slot(ops):
     c = Case(2, 20, 128, 64, E=3, rank=16, mods=2)
     c.x[13:] = math.nan
     _check_experts(ops, c, counts, None, "silu", True, "bf16", extra=7)
+
+
+@pytest.mark.parametrize("hit", [{0: 1}, {63: 2, 64: 3}, {511: 40}, {5: 1, 127: 20, 128: 33, 300: 7, 511: 1}])
+def test_many_experts(ops, hit):
+    counts = [hit.get(e, 0) for e in range(512)]
+    n = sum(counts)
+    c = Case(n, 50, 64, 96, E=512, rank=16, mods=2, bias=True)
+    rows = torch.randint(0, 50, (n,), generator=_gen(n), device="cuda").to(torch.int32)
+    _check_experts(ops, c, counts, rows, "silu", True, "bf16")
+
+
+def test_experts_mixed_types_and_modalities(ops):
+    c = Case(9, 40, 256, 96, E=3, rank=16, mods=4, io="bf16", lr="f32")
+    c.mod[::3] = 77                                         # no modality: text
+    rows = torch.randint(0, 40, (90,), generator=_gen(9), device="cuda").to(torch.int32)
+    got = ops.ExpertLinear(c.inv, c.wq, c.scale, c.ld, c.ru)(c.x, c.mod, _offsets([50, 0, 40]), rows=rows,
+                                                              out_dtype=torch.float32)
+    mod = torch.where(c.mod > 3, torch.zeros_like(c.mod), c.mod)
+    for e, a, b in ((0, 0, 50), (2, 50, 90)):
+        i = rows[a:b].long()
+        z, err = ref.layer(c.x[i], mod[i], c.inv, c.codes[e], c.scale[e], c.ld[e], c.ru[e])
+        ref.assert_close(got[a:b], *ref.finish(z, err, "none", False, None, torch.float32))
+
+
+@pytest.mark.parametrize("n", [6, 700])
+def test_rows_and_offsets_outside_their_range_are_clamped(ops, n):
+    c = Case(n, 20, 128, 64, E=2, rank=16, mods=2)
+    rows = torch.randint(0, 20, (n,), generator=_gen(n), device="cuda").to(torch.int32)
+    bad = rows.clone()
+    bad[::4] = torch.tensor([-1, 20, 2 ** 31 - 1, -2 ** 31], device="cuda")[torch.arange(len(bad[::4])) % 4].int()
+    lin = ops.ExpertLinear(c.inv, c.wq, c.scale, c.ld, c.ru)
+    first = torch.where((bad < 0) | (bad >= 20), torch.zeros_like(bad), bad)
+    want = lin(c.x, c.mod, _offsets([2, n - 2]), rows=first)
+    off = torch.tensor([-5, 2, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    assert torch.equal(lin(c.x, c.mod, off, rows=bad), want)
 
 
 def test_experts_without_any_row(ops):
