@@ -472,6 +472,16 @@ masq_status fused_stage(const Fused& a, int stage) {
                                                 w.x_scale, w.u, w.u_hl, w.zero_base, w.n_zero, s,
                                                 w.pair));
         if (st != MASQ_OK) return st;
+    } else if ((stage & 1) && cmc && a.ex != nullptr &&
+               masq::epilogue_stage1_ok(w, a.c_in, a.rank, a.n_mod, to_dt(a.lr_dt))) {
+        // fp32 factors or a rank past 64: the experts' stage 1 over one expert
+        masq::TileExtra one{};
+        one.n_experts = 1;
+        st = from_hip(masq::launch_expert_stage1(a.x, to_dt(a.x_dt), a.modality, a.inv_smooth, a.l_down,
+                                                 to_dt(a.lr_dt), a.T, a.T, a.c_in, a.rank, a.n_mod, w.u,
+                                                 nullptr, w.q, w.x_scale, one, w.pair, s, w.zero_base,
+                                                 w.n_zero));
+        if (st != MASQ_OK) return st;
     } else if ((stage & 1) && cmc && masq::quant_down_ok(w, a.T, a.c_in)) {
         st = from_hip(masq::launch_quant_down(a.x, to_dt(a.x_dt), a.modality, a.inv_smooth, a.l_down,
                                               to_dt(a.lr_dt), a.T, a.c_in, a.rank, a.n_mod, w, s));

@@ -403,11 +403,30 @@ inline int64_t expert_tiles(int64_t n_slots, int64_t n_experts, int64_t bm) {
 }
 hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex);
 // Stage 1 of the experts' layer with a compensation: the codes and scales of
-// x's rows, and u by slot (u_hl optional: rank <= 64).
+// x's rows, and u by slot (u_hl optional: rank <= 64).  ex.offsets null: one
+// expert (n_experts = 1) of all slots.
 hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
                                 const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
                                 int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
-                                const TileExtra& ex, bool pair, hipStream_t s);
+                                const TileExtra& ex, bool pair, hipStream_t s,
+                                int* zero_ints = nullptr, int n_zero = 0);
+// The layer with an epilogue takes that stage 1, over one expert, where its
+// factors are fp32 or its rank passes 64 (us of the whole call, the layer's own
+// stage 1 / this one, 256 output channels): batches whose own down-projection
+// does not split K (T > 256) nearly always gain,
+//   rank 16, 1500 tokens   K 1024 20 / 14, 4096 53 / 26, 16384 201 / 104
+//   rank 64, 1500 tokens   K 1024 23 / 22, 4096 55 / 50, 16384 206 / 204
+//   rank 128 in bf16, 400  K 1024 24 / 15, 8192 111 / 43;
+// smaller ones while a workgroup's own walk along K, a pass for each modality
+// and, for the slower fp32 MFMA, a step for each 16 columns, is short:
+//   100 tokens, rank 16    K 4096 29 / 19, 8192 39 / 30, 16384 54 / 48 (17: 34 / 46)
+//   rank 64                K 1024 24 / 17, 2048 29 / 24, 4096 32 / 47
+//   rank 64, 3 modalities  K 1024 30 / 26, 2048 32 / 44
+//   rank 128 in bf16       K 1024 31 / 14, 8192 50 / 41, 16384 66 / 68 (17: 44 / 65)
+inline bool epilogue_stage1_ok(const Workspace& w, int64_t K, int rank, int n_mod, DT lr_dt) {
+    const int64_t blocks = lr_dt == DT::BF16 ? 1 : (rank <= 16 ? 1 : (rank <= 32 ? 2 : 4));
+    return w.n_kslices == 1 || (n_mod - 1) * blocks * K <= 8192;
+}
 
 // Routing: at most kRouteMaxExperts experts and kRouteMaxK choices a token.
 // blocks == 0: one workgroup takes the batch and no workspace is needed.

@@ -439,6 +439,8 @@ struct ExpertStage1 {
     int64_t downs;
     bool row_group;       // a row a workgroup
     bool pair;            // q row-paired (code_row / code_col)
+    int* zero_ints;       // cleared on the way (the layer's arrival counters)
+    int n_zero;
 };
 
 // A fragment's 16 rows lie a row apart in memory, so a load in the MFMA's own
@@ -470,8 +472,18 @@ __device__ __forceinline__ void expert_down_tile(const XT* __restrict__ x, const
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int K = a.K, r = a.r;
+    const int chunks = (r + 16 * RB - 1) / (16 * RB);
     GroupTile gt;
-    if (!group_tile<16 * RG>(ex, a.n_slots, linear_block(), (r + 16 * RB - 1) / (16 * RB), gt)) return;
+    if (ex.offsets == nullptr) {                             // one expert of all slots
+        const int64_t b = linear_block();
+        gt.expert = 0;
+        gt.tn = static_cast<int>(b % chunks);
+        gt.first = b / chunks * (16 * RG);
+        gt.end = min(gt.first + 16 * RG, a.n_slots);
+        if (gt.first >= a.n_slots) return;
+    } else if (!group_tile<16 * RG>(ex, a.n_slots, linear_block(), chunks, gt)) {
+        return;
+    }
     const int c0 = gt.tn * 16 * RB;
     const int nb = min(RB, (r - c0) >> 4);                   // 16-column blocks of the rank
     const int steps = (K + 31) >> 5, per = (steps + kEdWaves - 1) / kEdWaves;
@@ -595,6 +607,8 @@ __global__ __launch_bounds__(64 * kEdWaves, 4) void k_expert_stage1(const XT* __
     __shared__ __attribute__((aligned(16))) v4f red[kEdWaves][RG * RB * 64];
     __shared__ int list[64];
     const int64_t b = linear_block() - a.downs;
+    if (b == 0)
+        for (int i = threadIdx.x; i < a.n_zero; i += 64 * kEdWaves) a.zero_ints[i] = 0;
     if (b < 0) {
         expert_down_tile<XT, LT, RG, RB, U>(x, l_down, a, ex, red, list);
     } else if (a.row_group) {
@@ -712,9 +726,10 @@ static hipError_t launch_stage1_t(const void* x, const void* l_down, ExpertStage
 hipError_t launch_expert_stage1(const void* x, DT x_dt, const int32_t* mod, const float* inv_s,
                                 const void* l_down, DT lr_dt, int64_t T, int64_t n_slots, int64_t K,
                                 int rank, int n_mod, float* u, uint8_t* u_hl, int8_t* q, float* x_scale,
-                                const TileExtra& ex, bool pair, hipStream_t s) {
+                                const TileExtra& ex, bool pair, hipStream_t s, int* zero_ints,
+                                int n_zero) {
     ExpertStage1 a{mod, inv_s, n_slots, T, static_cast<int>(K), rank, n_mod, u, u_hl, q, x_scale, 0,
-                   T < kRowsPerWaveMinT, pair};
+                   T < kRowsPerWaveMinT, pair, zero_ints, n_zero};
 #define MASQ_RB(XT, LT)                                                                             \
     (rank <= 16 ? launch_stage1_t<XT, LT, 1>(x, l_down, a, ex, s)                                   \
                 : (rank <= 32 ? launch_stage1_t<XT, LT, 2>(x, l_down, a, ex, s)                     \

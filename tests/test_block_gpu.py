@@ -97,6 +97,26 @@ def test_layer_epilogue(ops, T, K, N, rank, mods, io, bits, act, gated, bias, re
     ref.assert_close(got, *ref.finish(z, e, act, gated, c.res, DT[io]))
 
 
+@pytest.mark.parametrize("T,K,N,rank,mods,io,lr", [
+    # down-projections of fp32 factors and of ranks past 64: batches and rows on
+    # both sides of the choice between the two first stages, odd batches
+    (17, 64, 64, 16, 2, "f32", "f32"), (1, 1040, 48, 32, 3, "f32", "f32"), (100, 8192, 64, 16, 2, "f32", "f32"),
+    (99, 8256, 64, 16, 2, "f32", "f32"), (33, 2048, 96, 64, 2, "bf16", "f32"), (33, 2112, 96, 64, 2, "bf16", "f32"),
+    (255, 1040, 272, 48, 4, "f32", "f32"), (257, 1040, 272, 48, 4, "f32", "f32"),
+    (301, 4160, 64, 256, 2, "bf16", "bf16"),
+    (77, 4096, 80, 80, 3, "f32", "bf16"), (77, 4160, 80, 80, 3, "f32", "bf16"), (2049, 128, 32, 128, 2, "bf16", "bf16"),
+    (4097, 64, 48, 256, 2, "f32", "f32"), (301, 18944, 32, 16, 2, "bf16", "f32"),
+])
+def test_compensations_of_fp32_factors_and_high_ranks(ops, T, K, N, rank, mods, io, lr):
+    c = Case(T + K + rank, T, K, N, rank=rank, mods=mods, io=io, lr=lr, bias=True, residual=True, width=N)
+    lin = ops.Linear(c.inv, c.wq, c.scale, c.ld, c.ru)
+    ws = torch.full((ops.workspace_bytes(T, K, N, rank, mods),), 255, dtype=torch.uint8, device="cuda")  # dirty
+    got = lin.fused(c.x, c.mod, bias=c.bias, act="silu", residual=c.res, workspace=ws)
+    z, e = ref.layer(c.x, c.mod, c.inv, c.codes, c.scale, c.ld, c.ru, c.bias)
+    ref.assert_close(got, *ref.finish(z, e, "silu", False, c.res, DT[io]))
+    assert torch.equal(got, lin.fused(c.x, c.mod, bias=c.bias, act="silu", residual=c.res, workspace=ws))
+
+
 @pytest.mark.parametrize("T,K,N", [(1, 512, 256), (16, 2048, 512), (40, 512, 512), (400, 1024, 4096),
                                    (50, 8192, 528), (128, 18944, 512), (2304, 320, 6176)])
 def test_epilogue_of_nothing_is_the_layer(ops, T, K, N):
