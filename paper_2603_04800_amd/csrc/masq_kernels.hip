@@ -2239,16 +2239,25 @@ __device__ __forceinline__ void gemm_epilogue_extra(
                         if (!(present & (1u << m))) continue;
                         const bool live = tmod == m;
                         const uint8_t* base = sm.buf + c * chunk_bytes;
+                        int crow[NJ];
 #pragma unroll
-                        for (int j = 0; j < NJ; ++j) {
-                            const int crow = wn * 32 * NJ + 32 * j + (lane & 31);
-                            if (staged)
-                                ybs[j] = Cmc<LT>::from_lds(base, base + kU + p * kR, min(64, r - 64 * c), trow,
-                                                           crow, live, lane, ybs[j]);
-                            else
-                                ybs[j] = Cmc<LT>::from_global(u, r_up + static_cast<int64_t>(m - 1) * N * r,
-                                                              live && row0 + trow < T, row0 + trow,
-                                                              min(col0 + crow, N - 1), r, 64 * c, lane, ybs[j]);
+                        for (int j = 0; j < NJ; ++j) crow[j] = wn * 32 * NJ + 32 * j + (lane & 31);
+                        if (sizeof(LT) == 4 && staged) {
+                            // the blocks' independent MFMA chains side by side (4096 x
+                            // 2048 -> 8192 in fp32, rank 64: 328 us one by one, 273 so)
+                            if constexpr (sizeof(LT) == 4)
+                                Cmc<LT>::template from_lds_multi<NJ>(base, base + kU + p * kR, min(64, r - 64 * c),
+                                                                     trow, crow, live, lane, ybs);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < NJ; ++j)
+                                ybs[j] = staged
+                                             ? Cmc<LT>::from_lds(base, base + kU + p * kR, min(64, r - 64 * c), trow,
+                                                                 crow[j], live, lane, ybs[j])
+                                             : Cmc<LT>::from_global(u, r_up + static_cast<int64_t>(m - 1) * N * r,
+                                                                    live && row0 + trow < T, row0 + trow,
+                                                                    min(col0 + crow[j], N - 1), r, 64 * c, lane,
+                                                                    ybs[j]);
                         }
                         ++p;
                     }
