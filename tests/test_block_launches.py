@@ -65,6 +65,21 @@ def test_launches_stay_within_the_thread_limit(record, call):
     assert status == 0 and launches, (call, status, launches)
 
 
+@pytest.mark.parametrize("call,launches", [
+    # fp32 factors and ranks past 64: one launch before the product, also where
+    # both of its roles together pass one launch dimension
+    (f"epilogue 67000000 64 16 256 2 {F32} {F32} 8 0", 2), (f"epilogue 67108860 16 16 64 4 {BF16} {F32} 8 0", 2),
+    (f"epilogue 67108860 64 32 128 2 {BF16} {BF16} 4 17", 2), (f"epilogue 333 1040 2000 16 2 {F32} {F32} 8 2", 2),
+    # a split K and a long walk: the layer's own quantisation and down-projection
+    (f"epilogue 20 18944 1024 64 2 {F32} {F32} 8 0", 3),
+])
+def test_first_stage_of_fp32_factors_and_high_ranks(record, call, launches):
+    status, la = record([call])[0]
+    assert status == 0 and len(la) == launches, (call, status, la)
+    for x, y, z, threads in la:
+        assert x * threads < 2 ** 32 and y * z < 2 ** 16 and x * y * z > 0
+
+
 def test_host_code_under_sanitizers(tmp_path_factory):
     clang = "/opt/rocm/llvm/bin/clang"
     if not os.path.exists(clang):
