@@ -86,10 +86,14 @@ __device__ __forceinline__ int64_t slot_row(const TileExtra& ex, int64_t slot) {
 // 1 / (1 + exp(-z)) from v_exp_f32 and v_rcp_f32 (one unit in the last place
 // each).  Results that are rounded to bf16 take -z log2 e as one product, off by
 // |z| 2^-24; fp32 results add the product's own error and the next bits of
-// log2 e.  An exponential that overflows has the reciprocal 0, the limit.
+// log2 e.  An exponential that overflows has the reciprocal 0, the limit.  The
+// correction is a difference, which a product past fp32's range would make
+// infinity less infinity, so fp32 results take z within +-128, past which the
+// function is 1 or below the smallest normal number whatever z is.
 template <bool EXACT>
 __device__ __forceinline__ float logistic(float z) {
     constexpr float kL = -1.44269504088896341f, kLo = -1.92596299e-8f, kLn2 = 0.69314718055994531f;
+    if constexpr (EXACT) z = __builtin_amdgcn_fmed3f(z, -128.f, 128.f);
     const float t = z * kL;
     float e = __builtin_amdgcn_exp2f(t);
     if constexpr (EXACT) e *= fmaf(fmaf(z, kLo, fmaf(z, kL, -t)), kLn2, 1.f);

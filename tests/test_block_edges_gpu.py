@@ -1,0 +1,57 @@
+"""The operators around the quantised layer on the GPU, where test_block_gpu.py does
+not reach."""
+import math
+
+import pytest
+import torch
+
+import block_reference as ref
+from test_block_gpu import DT
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2603_04800_amd import ops as o
+    return o
+
+
+# ------------------------------------------------------------------ activations
+# |z| from where every activation is z or 0 to fp32 working precision, past 7e12,
+# where z^3 leaves fp32, to past 2.4e38, where z log2 e does
+FAR = [200.0, 1e3, 1e7, 6.5e12, 8e12, 1e13, 1e20, 1e30, 2.3e38, 2.5e38, 3e38]
+
+
+@pytest.mark.parametrize("T", [8, 300])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_activations_far_from_zero(ops, act, io, gated, T):
+    """act(z) is z for z far above zero and 0 far below.  z carries 3 u of the
+    product; logistic and erfc are within 8 u of 1 there (exp, reciprocal, their
+    products); gating and the output round once more.  The last pair of channels
+    overflows fp32: the infinity above stays one."""
+    K, per = 64, 2 if gated else 1
+    far = FAR + [1e42]
+    z = torch.tensor([s * v for v in far for s in (1.0, -1.0)] + [0.0] * 8, dtype=torch.float64, device="cuda")
+    N = per * z.numel()
+    x = torch.ones((T, K), device="cuda", dtype=DT[io])
+    x[-1] = 0                                               # a row of zeros beside them
+    codes = torch.full((N, K), 127, device="cuda", dtype=torch.int8)
+    codes[per:per * len(far) * 2:2 * per] = -127            # (a gate's negative; its up channel stays positive)
+    scale = torch.full((N,), 0.5 / (127 * K), device="cuda")
+    scale[::per] = (z.abs() / (127 * K)).clamp(max=1e38).float()
+    inv, mod = torch.ones((1, K), device="cuda"), torch.zeros(T, device="cuda", dtype=torch.int32)
+    got = ops.Linear(inv, codes, scale).fused(x, mod, act=act, gated=gated).double()
+    want, _ = ref.layer(x, mod, inv, codes, scale, None, None)
+    want = torch.where(want[:, ::per] > 0, want[:, ::per], torch.zeros_like(want[:, ::per])) * (0.5 if gated else 1.0)
+    n = 2 * len(FAR)
+    want, over = want[:, :n], got[:, n:n + 2]
+    # (codes 127 and steps of 1 / 127: the up channel is 0.5 to 3 u)
+    err = want * (ref.U * 16 + torch.finfo(DT[io]).eps / 2 * 1.01) + 1e-37
+    want, err = want[:-1], err[:-1]
+    ref.assert_close(got[:-1, :n], want, err)
+    assert (over[:-1, 0] == math.inf).all()
+    assert not got[-1].isnan().any() and not got[-1].any()
+    assert not got[:, n + 2:].any()
