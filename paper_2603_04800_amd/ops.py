@@ -802,13 +802,16 @@ class ExpertLinear:
             raise ValueError("wq does not match inv_smooth's width")
         self.width = self.c_out // 2 if gated else self.c_out
         E, M, N = self.n_experts, self.n_mod, self.c_out
-        self.rank = l_down.shape[2] if l_down is not None and l_down.dim() == 4 else 0
         _need(inv_smooth, torch.float32, "inv_smooth")
         _shaped(w_scale, (E, N), torch.float32, "w_scale")
         _shaped(bias, (E, N), torch.float32, "bias")
-        if self.rank:
-            if r_up is None:
-                raise ValueError("l_down needs r_up")
+        if (l_down is None) != (r_up is None):
+            raise ValueError("l_down and r_up come together")
+        self.rank = 0
+        if l_down is not None:
+            if l_down.dim() != 4:
+                raise ValueError(f"l_down must be [{E}][{M - 1}][rank][{self.c_in}], got {list(l_down.shape)}")
+            self.rank = l_down.shape[2]
             _shaped(l_down, (E, M - 1, self.rank, self.c_in), l_down.dtype, "l_down")
             _shaped(r_up, (E, M - 1, N, self.rank), l_down.dtype, "r_up")
 
