@@ -637,6 +637,21 @@ class Linear:
         return BoundLinear(self, x, modality, out, workspace, stream)
 
 
+    def _check_arrays(self):
+        """Types and shapes of the layer's arrays, which the C call cannot see."""
+        M, N, K, r = self.n_mod, self.c_out, self.c_in, self.rank
+        if self.wq.dtype not in (torch.int8, torch.uint8):
+            raise TypeError(f"wq must be torch.int8 or packed torch.uint8, got {self.wq.dtype}")
+        _need(self.inv_smooth, torch.float32, "inv_smooth")
+        _shaped(self.w_scale, (N,), torch.float32, "w_scale")
+        if M == 1 or (self.l_down is not None and self.l_down.dim() == 3 and r == 0):
+            return                                          # no compensation: what is there is not read
+        if (self.l_down is None) != (self.r_up is None):
+            raise ValueError("l_down and r_up come together")
+        if self.l_down is not None:
+            _shaped(self.l_down, (M - 1, r, K), self.l_down.dtype, "l_down")
+            _shaped(self.r_up, (M - 1, N, r), self.l_down.dtype, "r_up")
+
     def fused(self, x, modality, bias=None, act="none", gated=False, residual=None, out=None,
               out_dtype=None, workspace=None, stream=None):
         """The layer with bias [N] f32, activation and residual in its
@@ -652,6 +667,7 @@ class Linear:
         code = _act(act, gated)
         if x.dim() != 2 or x.shape[1] != self.c_in:
             raise ValueError(f"x must be [T][{self.c_in}]")
+        self._check_arrays()
         T = x.shape[0]
         shape = (T, self.c_out // 2 if gated else self.c_out)
         dev = _device_of(x=x, modality=modality, wq=self.wq, inv_smooth=self.inv_smooth,
