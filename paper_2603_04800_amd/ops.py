@@ -828,6 +828,7 @@ class ExpertLinear:
             if l_down.dim() != 4:
                 raise ValueError(f"l_down must be [{E}][{M - 1}][rank][{self.c_in}], got {list(l_down.shape)}")
             self.rank = l_down.shape[2]
+        if self.rank:                                       # (of rank 0: not read)
             _shaped(l_down, (E, M - 1, self.rank, self.c_in), l_down.dtype, "l_down")
             _shaped(r_up, (E, M - 1, N, self.rank), l_down.dtype, "r_up")
 

@@ -30,6 +30,7 @@ def test_expert_factors_come_together():
 def test_expert_factors_that_fit():
     assert _experts(torch.ones(3, 1, 16, 64), torch.ones(3, 1, 32, 16)).rank == 16
     assert _experts(torch.ones(3, 1, 0, 64), torch.ones(3, 1, 32, 0)).rank == 0
+    assert _experts(torch.ones(3, 1, 0, 64), torch.ones(3, 1, 32, 16)).rank == 0          # not read
     assert _experts(None, None).rank == 0
 
 
