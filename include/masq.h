@@ -255,6 +255,8 @@ masq_status masq_linear_epilogue(const void* x, masq_dtype x_dt, const int32_t* 
  *   slot_modality [T top_k] (given with modality [T], or both NULL): the
  *       modality of each slot's token, 0 past the last choice
  * 1 <= n_experts <= 512, 1 <= top_k <= min(n_experts, 16), T top_k < 2^31.
+ * T == 0 writes nothing, offsets neither: a caller that goes on to read them
+ * clears them itself (ops.route_experts does, on the call's stream).
  * workspace: masq_route_experts_workspace_bytes(...) bytes (0 for small
  * batches: may then be NULL), 256-byte aligned, contents need not be
  * initialised, not shared by concurrent calls.

@@ -499,8 +499,9 @@ def bind_route_experts(logits, top_k, renormalize=True, modality=None, stream=No
     r = Routing(new((T, top_k), i32), new((T, top_k), torch.float32), new((E + 1,), i32),
                 new((T * top_k,), i32), new((T, top_k), i32),
                 new((T * top_k,), i32) if modality is not None else None)
-    if T == 0:
-        r.offsets.zero_()
+    if T == 0:                                              # (the C call writes nothing then)
+        with torch.cuda.stream(stream):
+            r.offsets.zero_()
     need = int(_lib.masq_route_experts_workspace_bytes(T, E))
     ws = new((need,), torch.uint8) if need else None
     args = (_ptr(logits), _dt(logits), _ptr(modality), T, E, top_k, 1 if renormalize else 0,

@@ -55,3 +55,20 @@ def test_activations_far_from_zero(ops, act, io, gated, T):
     assert (over[:-1, 0] == math.inf).all()
     assert not got[-1].isnan().any() and not got[-1].any()
     assert not got[:, n + 2:].any()
+
+
+# ------------------------------------------------------------------ routing
+def test_empty_routing_writes_its_offsets_on_the_calls_stream(ops):
+    logits = torch.empty((0, 8), device="cuda")
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):                              # memory of s that s itself fills, late
+        torch.cuda._sleep(200_000_000)
+        junk = torch.full((9,), -1, dtype=torch.int32, device="cuda")
+        at = junk.data_ptr()
+        del junk
+    r = ops.route_experts(logits, 2, stream=s)
+    assert r.offsets.data_ptr() == at
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert r.offsets.tolist() == [0] * 9
