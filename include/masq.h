@@ -277,7 +277,8 @@ masq_status masq_linear_epilogue(const void* x, masq_dtype x_dt, const int32_t* 
  *   rows [n_slots] in [0, T) at the experts' slots, offsets [n_experts + 1]
  *   ascending in [0, n_slots]: DEVICE arrays that the host never reads.
  *   (Other values are memory-safe, but not a supported input: rows outside
- *   [0, T) read row 0, offsets are clamped.)
+ *   [0, T) read row 0, offsets are clamped, and rows of y may be left as they
+ *   were where offsets do not ascend.)
  *   y [n_slots][c_out, or c_out / 2 where gated]
  * T == 0 or n_slots == 0 is a no-op.  workspace:
  * masq_expert_linear_workspace_bytes(...) bytes, 256-byte aligned, not shared

@@ -398,7 +398,7 @@ hipError_t launch_gemm_stream_epilogue(const StreamGemm& g, const TileExtra& ex)
 // g.x_scale and g.q by row of x, g.u by slot; plain codes, one slice).
 // expert_tiles: the most tiles of bm rows that the slots can make, whatever
 // their distribution.
-inline int64_t expert_tiles(int64_t n_slots, int64_t n_experts, int64_t bm) {
+__host__ __device__ inline int64_t expert_tiles(int64_t n_slots, int64_t n_experts, int64_t bm) {
     return n_slots / bm + (n_slots < n_experts ? n_slots : n_experts);
 }
 hipError_t launch_gemm_experts(const TileGemm& g, const TileExtra& ex);

@@ -32,7 +32,9 @@ constexpr int kExpertGroup = 3;
 // The tile of workgroup `block`: every wave counts the experts' tiles of BM
 // rows, a lane an expert, places the workgroup among them as tile_coords_at
 // does, and finds the expert that holds its row of tiles.  False past the last
-// tile (the grid is sized for the most tiles that n slots can make).
+// tile (the grid is sized for the most tiles that n slots can make).  Offsets
+// that do not ascend can ask for more tiles than that, more than an int counts:
+// they get none.
 template <int BM>
 __device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64_t block, int tiles_n,
                                            GroupTile& out) {
@@ -52,13 +54,16 @@ __device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64
     };
     int lo, hi;
     int incl = scan(count(lane, lo, hi));
-    int total = __builtin_amdgcn_readlane(incl, 63);
+    int64_t total = __builtin_amdgcn_readlane(incl, 63);
     for (int b = 64; b < ex.n_experts; b += 64) {
         int l2, h2;
         total += __builtin_amdgcn_readlane(scan(count(b + lane, l2, h2)), 63);
     }
+    // (64 lanes' tiles: at most half of them can start over, 32 n / BM + 64)
+    if (total > expert_tiles(n, ex.n_experts, BM)) return false;
     int tm;
-    if (!tile_coords_at<kExpertGroup>(static_cast<int>(block), total, tiles_n, tm, out.tn)) return false;
+    if (!tile_coords_at<kExpertGroup>(static_cast<int>(block), static_cast<int>(total), tiles_n, tm, out.tn))
+        return false;
     int before = 0, b = 0;
     for (;;) {
         const int here = __builtin_amdgcn_readlane(incl, 63);

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import block_reference as ref
-from test_block_gpu import DT
+from test_block_gpu import DT, Case, _gen
 
 pytestmark = pytest.mark.gpu
 
@@ -57,7 +57,7 @@ def test_activations_far_from_zero(ops, act, io, gated, T):
     assert not got[:, n + 2:].any()
 
 
-# ------------------------------------------------------------------ routing
+# ------------------------------------------------------------------ routing and offsets
 def test_empty_routing_writes_its_offsets_on_the_calls_stream(ops):
     logits = torch.empty((0, 8), device="cuda")
     s = torch.cuda.Stream()
@@ -72,3 +72,15 @@ def test_empty_routing_writes_its_offsets_on_the_calls_stream(ops):
     s.synchronize()
     torch.cuda.synchronize()
     assert r.offsets.tolist() == [0] * 9
+
+
+@pytest.mark.parametrize("n,K,N", [(400, 128, 64), (3000, 64, 3104)])
+def test_offsets_that_do_not_ascend_stay_within_the_rows(ops, n, K, N):
+    """Experts that claim the same slots make more tiles than the slots can: no
+    row is written, and none past them."""
+    c = Case(n, 20, K, N, E=6, rank=16, mods=2)
+    rows = torch.randint(0, 20, (n,), generator=_gen(n), device="cuda").to(torch.int32)
+    off = torch.tensor([0, n, 0, n, 0, n, 0], dtype=torch.int32, device="cuda")
+    buf = torch.full((n + 64, N), 7.25, dtype=torch.bfloat16, device="cuda")
+    ops.ExpertLinear(c.inv, c.wq, c.scale, c.ld, c.ru)(c.x, c.mod, off, rows=rows, out=buf[:n])
+    assert (buf == 7.25).all()
