@@ -42,8 +42,10 @@ if ROOT not in sys.path:
 
 INT8_PEAK_TOPS = 5000.0      # MI355X dense int8 MFMA
 HBM_PEAK_GBS = 8000.0        # MI355X HBM3E
-KERNEL_SOURCES = tuple("paper_2603_04800_amd/csrc/" + f for f in (
-    "masq_kernels.hip", "masq_tile.hip", "masq_tile.h", "masq_epilogue.h", "masq_quant.h"))
+# what the library is compiled from: the profiles' hash
+KERNEL_SOURCES = tuple("paper_2603_04800_amd/csrc/" + f
+                       for f in sorted(os.listdir(os.path.join(ROOT, "paper_2603_04800_amd", "csrc")))
+                       if f.endswith((".hip", ".h")) and f != "masq_probe.hip")
 
 
 def log(msg):
