@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import block_reference as ref
-from test_block_gpu import DT, Case, _gen
+from test_block_gpu import DT, Block, Case, _gen, _offsets, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -84,3 +84,99 @@ def test_offsets_that_do_not_ascend_stay_within_the_rows(ops, n, K, N):
     buf = torch.full((n + 64, N), 7.25, dtype=torch.bfloat16, device="cuda")
     ops.ExpertLinear(c.inv, c.wq, c.scale, c.ld, c.ru)(c.x, c.mod, off, rows=rows, out=buf[:n])
     assert (buf == 7.25).all()
+
+
+# ------------------------------------------------------------------ the first stage's forms
+def _dirty(ops, T, n, K, rank, mods):
+    need = ops.raw().masq_expert_linear_workspace_bytes(T, n, K, rank, mods)
+    return torch.full((need,), 255, dtype=torch.uint8, device="cuda")           # NaN throughout
+
+
+@pytest.mark.parametrize("counts,T,K,rank,mods,io,lr", [
+    # slots in groups of 32 (past 512 groups of 16) and of 64 (past 1024), one and
+    # two rank blocks, then four; experts that end inside a group, rows that end
+    # inside a step
+    ([4001, 0, 17, 5003], 500, 96, 16, 2, "bf16", "bf16"), ([3000, 33, 6100], 0, 80, 32, 3, "bf16", "bf16"),
+    ([9100, 1], 300, 144, 16, 4, "f32", "f32"), ([2222, 7001], 0, 64, 32, 2, "bf16", "f32"),
+    ([8200, 9001, 40], 700, 80, 16, 3, "bf16", "bf16"), ([16999, 0, 31], 0, 96, 32, 4, "bf16", "bf16"),
+    ([5, 17001], 400, 112, 32, 2, "f32", "f32"), ([17100], 200, 64, 16, 2, "f32", "bf16"),
+    ([700, 16900], 0, 80, 16, 3, "bf16", "f32"),
+    ([9001, 70], 333, 80, 48, 3, "bf16", "bf16"), ([10, 9300], 0, 96, 64, 2, "f32", "f32"),
+])
+def test_every_form_of_the_first_stage(ops, counts, T, K, rank, mods, io, lr):
+    E, n, N = len(counts), sum(counts), 32
+    c = Case(n + K, T or n, K, N, E=E, rank=rank, mods=mods, io=io, lr=lr, bias=True)
+    rows = torch.randint(0, T, (n,), generator=_gen(n), device="cuda").to(torch.int32) if T else None
+    at = rows.long() if T else torch.arange(n, device="cuda")
+    lin = ops.ExpertLinear(c.inv, c.wq, c.scale, c.ld, c.ru, bias=c.bias, act="silu")
+    got = lin(c.x, c.mod, _offsets(counts), rows=rows, workspace=_dirty(ops, T or n, n, K, rank, mods))
+    lo = 0
+    for e, cnt in enumerate(counts):
+        i = at[lo:lo + cnt]
+        if cnt:
+            z, err = ref.layer(c.x[i], c.mod[i], c.inv, c.codes[e], c.scale[e], c.ld[e], c.ru[e], c.bias[e])
+            ref.assert_close(got[lo:lo + cnt], *ref.finish(z, err, "silu", False, None, DT[io]))
+        lo += cnt
+
+
+@pytest.mark.parametrize("T,K,rank,mods,io,lr", [
+    # the same forms over a layer's own rows (one expert)
+    (9001, 80, 16, 3, "f32", "f32"), (8999, 96, 32, 2, "bf16", "f32"), (17003, 64, 16, 2, "bf16", "f32"),
+    (17001, 144, 32, 4, "f32", "f32"), (9003, 80, 80, 3, "bf16", "bf16"),
+])
+def test_every_form_of_the_first_stage_over_a_layers_rows(ops, T, K, rank, mods, io, lr):
+    N = 32
+    c = Case(T, T, K, N, rank=rank, mods=mods, io=io, lr=lr, bias=True, residual=True, width=N)
+    ws = torch.full((ops.workspace_bytes(T, K, N, rank, mods),), 255, dtype=torch.uint8, device="cuda")
+    got = ops.Linear(c.inv, c.wq, c.scale, c.ld, c.ru).fused(c.x, c.mod, bias=c.bias, act="silu", residual=c.res,
+                                                             workspace=ws)
+    z, err = ref.layer(c.x, c.mod, c.inv, c.codes, c.scale, c.ld, c.ru, c.bias)
+    ref.assert_close(got, *ref.finish(z, err, "silu", False, c.res, DT[io]))
+
+
+# ------------------------------------------------------------------ layers that split K over 256 x 256 tiles
+@pytest.mark.parametrize("T,K,N,rank,mods,io,bits,act,gated", [
+    (257, 18944, 3584, 64, 2, "bf16", 8, "none", False), (300, 18944, 3584, 16, 3, "f32", 8, "silu", True),
+    (384, 18944, 3584, 64, 2, "bf16", 4, "gelu", False), (401, 28672, 2048, 32, 2, "bf16", 8, "gelu_tanh", True),
+])
+def test_layers_whose_own_product_splits_k(ops, T, K, N, rank, mods, io, bits, act, gated):
+    width = N // 2 if gated else N
+    c = Case(T + K, T, K, N, rank=rank, mods=mods, io=io, bits=bits, bias=True, residual=True, width=width)
+    lin = ops.Linear(c.inv, c.wq, c.scale, c.ld, c.ru)
+    got = lin.fused(c.x, c.mod, bias=c.bias, act=act, gated=gated, residual=c.res)
+    z, e = ref.layer(c.x, c.mod, c.inv, c.codes, c.scale, c.ld, c.ru, c.bias)
+    ref.assert_close(got, *ref.finish(z, e, act, gated, c.res, DT[io]))
+    text = c.mod == 0
+    assert torch.equal(lin.fused(c.x, c.mod)[text], lin(c.x, c.mod)[text])
+
+
+# ------------------------------------------------------------------ replays on the inputs captured
+def test_replays_repeat_the_eager_result(ops):
+    blocks = [Block(ops, s, T, 8, 2, 256, 128) for s, T in ((3, 9), (30, 300))]
+    lin = [ops.Linear(b.dn.inv, b.dn.wq[0], b.dn.scale[0], b.dn.ld[0], b.dn.ru[0]) for b in blocks]
+    c = Case(5, 64, 4096, 96, rank=16, mods=2, bias=True, residual=True, width=96)   # slices and their counters
+    split = ops.Linear(c.inv, c.wq, c.scale, c.ld, c.ru)
+
+    def all_of(b, l):
+        y = b()
+        return (y, l.fused(y[:, :128].contiguous(), b.up.mod, act="silu", residual=b.res),
+                split.fused(c.x, c.mod, bias=c.bias, act="gelu", residual=c.res))
+
+    eager = [all_of(b, l) for b, l in zip(blocks, lin)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [], []
+    for b, l in zip(blocks, lin):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, stream=side):
+            outs.append(all_of(b, l))
+        graphs.append(gr)
+    for _ in range(3):
+        for gr, o, want, b, l in zip(graphs, outs, eager, blocks, lin):
+            for t in o:
+                t.fill_(math.nan)
+            gr.replay()
+            again = all_of(b, l)                            # eager work between the replays
+            torch.cuda.synchronize()
+            for got, w, a in zip(o, want, again):
+                assert torch.equal(got, w) and torch.equal(a, w)
