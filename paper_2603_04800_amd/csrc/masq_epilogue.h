@@ -23,10 +23,12 @@ __device__ __forceinline__ int group_edge(const TileExtra& ex, int e, int64_t n)
     return static_cast<int>(min(max(static_cast<int64_t>(ex.offsets[min(e, ex.n_experts)]), int64_t{0}), n));
 }
 
-// Rows of tiles that run together: those of one expert or two share a weight
-// (32768 slots over 64 experts, 2048 -> 2816: groups of 8 / 4 / 3 / 1 rows of 256 x 256
-// tiles 418 / 360 / 348 / 340 us the layer, on a persistent grid; 8 experts of 3584 -> 8192
-// 368 / 358 / 355 / 368).
+// Rows of tiles that run together: those of one expert or two share a weight.
+// Groups of 8 / 4 / 3 / 1 rows, us the layer: on 256 x 256 tiles 32768 slots over 64
+// experts, 2048 -> 2816 344 / 344 / 332 / 331 and 1408 -> 2048 251 / 258 / 241 / 248,
+// 16384 over 8, 3584 -> 8192 584 / 611 / 592 / 628 and 4096 -> 3584 330 / 334 / 338 /
+// 336; on smaller ones 8192 over 64, 2048 -> 2048 123 / 124 / 120 / 119 and over 16,
+// 2048 -> 4096 143 / 143 / 136 / 133.
 constexpr int kExpertGroup = 3;
 
 // The tile of workgroup `block`: every wave counts the experts' tiles of BM
@@ -108,11 +110,14 @@ template <bool EXACT>
 __device__ __forceinline__ float act_silu(float z) { return z * logistic<EXACT>(z); }
 // z Phi(z) = z erfc(-z / sqrt 2) / 2: erfc, unlike 1 + erf, keeps its relative
 // accuracy for negative z, where it is small.  Results that are rounded to bf16
-// take erfc(x) = t 2^(Q(t) - x^2 log2 e), t = 1 / (1 + x / 2), for x >= 0, with the
-// degree-9 Chebyshev interpolant Q of log2(erfc(x) e^(x^2) / t) over x in [0, 10],
-// off by 2.5e-7 of the value in fp32 (a residual may cancel the result, so the
-// output's rounding is no measure of what this may be off by).  4096 x
-// 3584 -> 37888 gated: 614 us where erfcf takes 709.
+// take erfc(x) = t 2^(Q(t) - x^2 log2 e), t = 1 / (1 + x / 2), for x >= 0 (the form
+// of Press et al., Numerical Recipes, 6.2), Q the degree-9 Chebyshev interpolant
+// in t of log2(erfc(x) e^(x^2) / t) over x in [0, 10], off by 1.2e-7 of the value.
+// The rounding of x^2 log2 e adds to that where the value is small: in all at most
+// (16 + 4 z^2) 2^-24 of it (found: 4.4e-7 up to z = -1, 1.2e-6 to -3, 8.3e-6 to -9,
+// 1.9e-5 to -13), and in absolute terms, what a residual that cancels the result
+// leaves, about 1e-7 for z < 0.  4096 x 3584 -> 37888 gated: 614 us where erfcf
+// takes 709.
 template <bool EXACT>
 __device__ __forceinline__ float act_gelu(float z) {
     if constexpr (EXACT) {
@@ -167,9 +172,10 @@ __device__ __forceinline__ void activate(int act, float (&v)[N]) {
 // element, so the two may be one array.  LDS operations of one wave execute in
 // order, so its buffer (32 rows of kEpiPitch floats) needs no synchronisation.
 //
-// The loop over the blocks is not unrolled (they move down a block a turn): a tile runs through this code once, so that its length is
-// paid in instruction fetches.  Fully unrolled, the products and epilogues of 4096 x
-// 3584 -> 37888 (gated) took 930 us where this form takes 593.
+// The loop over the blocks is not unrolled (they move down a block a turn): a
+// tile runs through this code once, so that its length is paid in instruction
+// fetches.  Fully unrolled, the products and epilogues of 4096 x 3584 -> 37888
+// (gated) took 930 us where this form takes 593.
 constexpr int kEpiPitch = 20;                               // 16 channels and 16 bytes
 template <typename YT, int NJ>
 __device__ __forceinline__ void finish_row(v16f (&yb)[NJ], const TileExtra& ex, const float* bias,
