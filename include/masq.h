@@ -49,6 +49,11 @@
  *    even; an all-zero row gives delta = 0 and zero codes; int32 accumulation
  *    is exact; dequantisation is fl(fl(float(acc) * delta_t) * w_scale[o]);
  *    bf16 outputs are one round-to-nearest-even of the fp32 result.
+ *    The compensation is summed in fp32.  With bf16 factors its products are
+ *    bf16 ones, and a smoothed row and its u = (x_t S_m^-1) L1^m may enter them
+ *    as a sum of two bf16 terms each, within 2^-16 of every value (so fp32
+ *    outputs hold the compensation to about 4e-6 of its terms); with fp32
+ *    factors both enter whole.  This holds for the experts' layer as well.
  *  - No C++ exception crosses this boundary.  The library's only global
  *    state is the static scratch of masq_linear_fused_noalloc (and its
  *    per-device address); every other call is safe concurrently if their

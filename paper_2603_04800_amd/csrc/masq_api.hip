@@ -511,7 +511,11 @@ masq_status fused_stage(const Fused& a, int stage) {
                                      a.rank, a.n_mod, a.r_up, to_dt(a.lr_dt), a.y, to_dt(a.y_dt), a.w4,
                                      w.dec_part, w.dec_tickets, -1, s},
                     *a.ex));
-            // (256 x 256 tiles split along K have no epilogue: 128 x 128 instead)
+            // 256 x 256 tiles split along K have no epilogue: whole 128 x 128 tiles
+            // instead, slower than a pass of its own over the outputs would be (us,
+            // the layer, the layer and such a pass for the residual, this: 18944 ->
+            // 3584, 257 tokens 81 / 82 / 105, 512 99 / 102 / 138; 28672 -> 8192, 257
+            // tokens 139 / 144 / 217; 8192 -> 8192, 512 tokens 72 / 78 / 65)
             const bool wide = w.tile.shape < 0 && w.gk_splits <= 1;
             const masq::TileGemm g{w.q, w.x_scale, a.wq, a.w_scale, a.T, a.c_in, a.c_out, a.modality,
                                    w.u, hl ? w.u_hl : nullptr, a.rank, a.n_mod, a.r_up, to_dt(a.lr_dt),
