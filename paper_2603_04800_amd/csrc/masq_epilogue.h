@@ -56,13 +56,14 @@ __device__ __forceinline__ bool group_tile(const TileExtra& ex, int64_t n, int64
     };
     int lo, hi;
     int incl = scan(count(lane, lo, hi));
-    int64_t total = __builtin_amdgcn_readlane(incl, 63);
+    // (64 lanes' tiles: at most half of them can start over, 32 n / BM + 64)
+    uint32_t total = static_cast<uint32_t>(__builtin_amdgcn_readlane(incl, 63));
     for (int b = 64; b < ex.n_experts; b += 64) {
         int l2, h2;
-        total += __builtin_amdgcn_readlane(scan(count(b + lane, l2, h2)), 63);
+        total = min(total + static_cast<uint32_t>(__builtin_amdgcn_readlane(scan(count(b + lane, l2, h2)), 63)),
+                    0x7FFFFFFFu);
     }
-    // (64 lanes' tiles: at most half of them can start over, 32 n / BM + 64)
-    if (total > expert_tiles(n, ex.n_experts, BM)) return false;
+    if (total > static_cast<uint32_t>(expert_tiles(n, ex.n_experts, BM))) return false;
     int tm;
     if (!tile_coords_at<kExpertGroup>(static_cast<int>(block), static_cast<int>(total), tiles_n, tm, out.tn))
         return false;
